@@ -117,61 +117,69 @@ def _quantise(x):
     return codes.to(torch.uint8).flatten(-2), s, z
 
 
-def _orders(d, dev):
-    """Channel of every nibble of a stored row (low nibble of byte 0 first), for keys and for values."""
+def _order(d, side, dev):
+    """Channel of every nibble of a stored row, low nibble of byte 0 first; side 0: keys, 1: values."""
     w = d // GROUP
     nib = torch.arange(d, device=dev)
-    word, i = nib // 8, nib % 8                                    # keys: word t w + group: channels 8 t .. 8 t + 7 of the group
-    key = (word % w) * GROUP + (word // w) * 8 + i
-    half, i = nib // 4, nib % 4                                    # values: half word g w + group: channels g, 8 + g, 16 + g, 24 + g of the group
-    return key, (half % w) * GROUP + i * 8 + half // w
+    if side == 0:                                                  # word t w + group: channels 8 t .. 8 t + 7 of the group
+        word, i = nib // 8, nib % 8
+        return (word % w) * GROUP + (word // w) * 8 + i
+    half, i = nib // 4, nib % 4                                    # half g w + group: channels g, 8 + g, 16 + g, 24 + g of the group
+    return (half % w) * GROUP + i * 8 + half // w
 
 
-def _pack(codes, s, z, order):
-    """A stored row: (code bytes [.., d/2], parameter bytes [.., d/8])."""
-    n = codes[..., order]
-    b = n[..., 0::2] | (n[..., 1::2] << 4)
-    par = torch.stack([s, z], -1).contiguous().view(torch.uint8).flatten(-2)
-    return b, par
+def _places(at, d, side):
+    """Bytes of a page's code area that the row of place `at` [..] of the page takes: [.., d/2]."""
+    byte = torch.arange(d // 2, device=at.device)
+    if side == 0:                                                  # keys: one row after the other
+        return at.unsqueeze(-1) * (d // 2) + byte
+    # values: blocks of 16 tokens, [token / 8][g][token / 2 % 4][group][token % 2] halves
+    w = d // GROUP
+    half, low = byte // 2, byte % 2
+    g, group = half // w, half % w
+    tok = (at % 16).unsqueeze(-1)
+    unit = ((tok // 8 * 32 + g * 4 + tok // 2 % 4) * w + group) * 2 + tok % 2
+    return (at // 16).unsqueeze(-1) * (8 * d) + unit * 2 + low
+
+
+def _areas(state, cache):
+    """Code and parameter areas of the pages: [pages, Hkv, 2, page d/2], [pages, Hkv, 2, page, d/8] bytes."""
+    c = state["case"]
+    cut = c["page"] * (c["d"] // 2)
+    blk = cache.view(cache.shape[0], c["Hkv"], 2, -1)
+    return blk[..., :cut], blk[..., cut:].unflatten(-1, (c["page"], c["d"] // 8))
 
 
 def _rows(state, pos):
     """Page and place of the tokens pos [B, m] of every sequence: [B, m] each."""
     page = state["case"]["page"]
-    table = state["pages"]
-    return torch.gather(table.long(), 1, pos // page), pos % page
+    return torch.gather(state["pages"].long(), 1, pos // page), pos % page
 
 
 def _plain_write(state, cache, k, v, pos):
     """Rows k, v [B, Hkv, m, d] into the pages at positions pos [B, m]."""
-    c = state["case"]
-    d, page = c["d"], c["page"]
-    blk = cache.view(cache.shape[0], c["Hkv"], 2, page * (d // 2 + d // 8))
-    codes = blk[..., :page * (d // 2)].unflatten(-1, (page, d // 2))
-    pars = blk[..., page * (d // 2):].unflatten(-1, (page, d // 8))
+    d = state["case"]["d"]
+    codes, pars = _areas(state, cache)
     pg, at = _rows(state, pos)
     for side, x in enumerate((k, v)):
-        b, par = _pack(*_quantise(x), _orders(d, x.device)[side])
-        codes[:, :, side][pg, :, at] = b.transpose(1, 2)
-        pars[:, :, side][pg, :, at] = par.transpose(1, 2)
+        code, s, z = _quantise(x)
+        n = code[..., _order(d, side, x.device)]
+        codes[:, :, side][pg.unsqueeze(-1), :, _places(at, d, side)] = (n[..., 0::2] | (n[..., 1::2] << 4)).permute(0, 2, 3, 1)
+        pars[:, :, side][pg, :, at] = torch.stack([s, z], -1).view(torch.uint8).flatten(-2).transpose(1, 2)
 
 
 def _plain_read(state, cache, pos):
     """Values of the tokens pos [B, m]: k, v [B, Hkv, m, d] float32."""
-    c = state["case"]
-    d, page = c["d"], c["page"]
-    blk = cache.view(cache.shape[0], c["Hkv"], 2, page * (d // 2 + d // 8))
-    codes = blk[..., :page * (d // 2)].unflatten(-1, (page, d // 2))
-    pars = blk[..., page * (d // 2):].unflatten(-1, (page, d // 8))
+    d = state["case"]["d"]
+    codes, pars = _areas(state, cache)
     pg, at = _rows(state, pos)
     got = []
     for side in (0, 1):
-        b = codes[:, :, side][pg, :, at].transpose(1, 2)                               # [B, Hkv, m, d/2]
+        b = codes[:, :, side][pg.unsqueeze(-1), :, _places(at, d, side)].permute(0, 3, 1, 2)          # [B, Hkv, m, d/2]
         par = pars[:, :, side][pg, :, at].transpose(1, 2).contiguous().view(torch.bfloat16).unflatten(-1, (-1, 2)).float()
         nib = torch.stack([b & 15, b >> 4], -1).flatten(-2).float()
-        order = _orders(d, b.device)[side]
         val = torch.empty_like(nib)
-        val[..., order] = nib
+        val[..., _order(d, side, b.device)] = nib
         got.append((par[..., 1:2] + par[..., 0:1] * val.unflatten(-1, (-1, GROUP))).flatten(-2))
     return got
 
@@ -447,17 +455,20 @@ def _stored64(state):
     d, page = c["d"], c["page"]
     raw = state["cache"][state["pages"].long()].permute(0, 2, 3, 1, 4)                    # [B, Hkv, 2, pages, bytes]
     cut = page * (d // 2)
-    bytes_, par = raw[..., :cut].unflatten(-1, (page, -1)).flatten(3, 4), raw[..., cut:].unflatten(-1, (page, -1)).flatten(3, 4)
+    codes, par = raw[..., :cut], raw[..., cut:].unflatten(-1, (page, -1)).flatten(3, 4)
     par = par.contiguous().view(torch.int16).to(torch.int32).bitwise_left_shift(16).view(torch.float32).double()
     s, z = par[..., 0::2], par[..., 1::2]
     w, chan = d // GROUP, torch.arange(d, device=DEV)
+    group, r, t = chan // GROUP, chan % GROUP, torch.arange(page, device=DEV).unsqueeze(1)
     got = []
     for side in (0, 1):
-        group, r = chan // GROUP, chan % GROUP
-        nib = ((r // 8) * w + group) * 8 + r % 8 if side == 0 else ((r % 8) * w + group) * 4 + r // 8
-        b = bytes_[:, :, side][..., nib // 2].to(torch.int32)
-        code = (b >> (4 * (nib % 2)).to(torch.int32)) & 15
-        got.append(z[:, :, side][..., group] + s[:, :, side][..., group] * code.double())
+        if side == 0:                                                                     # nibble of channel (group, r) of place t of a page
+            nib = t * d + ((r // 8) * w + group) * 8 + r % 8
+        else:
+            nib = t // 16 * 16 * d + ((t % 16 // 8 * 32 + r % 8 * 4 + t % 8 // 2) * w + group) * 8 + t % 2 * 4 + r // 8
+        b = codes[:, :, side][..., (nib // 2).flatten()].unflatten(-1, (page, d)).flatten(2, 3)
+        sh = (4 * (nib % 2)).to(torch.uint8).repeat(b.shape[2] // page, 1)
+        got.append(z[:, :, side][..., group] + s[:, :, side][..., group] * ((b >> sh) & 15).double())
     return got
 
 
