@@ -79,6 +79,7 @@ enum lot_device_flag {
     LOT_DEV_TIMEOUT = 4,   /* a bounded device-side wait gave up; results of the call are invalid */
     LOT_DEV_BOUNDS = 16,   /* bounds-check build only (compiled with -DLOT_DEBUG, lot_version() = 100100): an index of a
                               general-path or backward kernel fell outside its buffer; the access was skipped */
+    LOT_DEV_PAGE = 32,     /* a page table entry outside the pool, or a token behind the table's last page: skipped (see lot_cache4_write) */
     LOT_DEV_RECOMPUTED = 8 /* information only: the resident path could not represent the problem (see lot_path)
                               and the streamed kernels recomputed the call; the results are valid */
 };
@@ -291,6 +292,85 @@ LOT_API int lot_attention_fwd(const float *q, const float *k, const float *v,
                       const float *z, const float *beta,
                       int B, int H, int n, int d, int r, float eps, int iters,
                       float *out, lot_stream_t stream);
+
+/*
+ * Window attention with sinks, forward and backward: softmax attention for the layers the transport rule has no form for.  A doubly
+ * stochastic matrix that is lower triangular is the identity (Appendix "Bidirectional scope"), so the causal layers of a model that uses
+ * lot_attention_fwd_var for its cross-attention, and local layers beside its global ones, take these.
+ *
+ *   q, out, dout, dq [B,H,nq,d];  k, v, dk, dv [B,Hkv,nk,d], H a multiple of Hkv: query head h reads key head h / (H / Hkv)
+ *   key_len [B] int32 or NULL: keys j >= key_len[b] do not exist (NULL: nk; values outside [0, nk] are clamped)
+ *   q_start [B] int32 or NULL: query i of row b stands at position p = q_start[b] + i (NULL: nk - nq, the last query at the last key;
+ *   may be negative)
+ *   Query p sees key j where  j < key_len[b],  j <= p + right,  and  j >= p - left  or  j < sinks.
+ *   left, right < 0: no limit to that side.  Causal: right = 0.  sinks >= 0: the first keys stay visible when the window has passed them
+ *   (a class token, or the first tokens a decoder's softmax leans on).
+ *   out = sum_j P_ij v_j,  P_ij = exp(scale <q_i, k_j> - lse_i),  lse_i = log sum over the visible j (natural logarithm; [B,H,nq] float32).
+ *   A query that sees nothing gets out = 0, lse = -inf, and no gradient.
+ * Supported: d a multiple of 8 from 8 to 128, scale > 0 finite, nq, nk as n in the general conventions, B * H <= 32767.  nk = 0: every
+ * query sees nothing.
+ * Keys and values that no query of their batch row sees may hold anything, infinities and NaN too.  Of the others, queries, dout and
+ * values must be finite: a value that is not may reach queries that do not see it.
+ * Scores, softmax statistics and sums are float32; bf16 tensors: P and the score gradients are rounded to bf16 for their products.
+ * status: device int32 or NULL; the flags of enum lot_device_flag are OR-ed into it (clear it first).  LOT_DEV_TIMEOUT: results invalid.
+ * out may not overlap the inputs.
+ */
+LOT_API size_t lot_window_fwd_workspace_bytes(int dtype, int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks);
+LOT_API int lot_window_fwd(const void *q, const void *k, const void *v, const int32_t *key_len, const int32_t *q_start,
+                   int dtype, int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks, float scale,
+                   void *out, float *lse /* or NULL */, int32_t *status,
+                   void *ws, size_t ws_bytes, lot_stream_t stream);
+
+/*
+ * lot_window_bwd -- gradients of lot_window_fwd: dout = d(loss)/d(out) gives d(loss)/d(q, k, v); those of a key head are summed over its
+ * query heads.  out, lse: what the forward gave.  Rows of dk, dv that no query sees are zero.
+ */
+LOT_API size_t lot_window_bwd_workspace_bytes(int dtype, int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks);
+LOT_API int lot_window_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *dout,
+                   const int32_t *key_len, const int32_t *q_start,
+                   int dtype, int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks, float scale,
+                   void *dq, void *dk, void *dv, int32_t *status,
+                   void *ws, size_t ws_bytes, lot_stream_t stream);
+
+/*
+ * A cache of keys and values in 4 bits, in pages, and the attention that reads it (the decoder's serving form of the above).
+ *
+ *   cache  [num_pages][Hkv][2: keys, values][page_size * (d/2 + d/8)] bytes: lot_cache4_bytes(...) bytes in all, 16-byte aligned
+ *   pages  [B, max_pages] int32: pages[b][i] holds the tokens i * page_size .. of sequence b.  Entries of pages that a call has no token
+ *          in are never read.  An entry outside [0, num_pages): its tokens are not written, read as zeros, and not attended to
+ *          (LOT_DEV_PAGE).
+ *   Groups of 32 channels of a token and head share a scale and a least value, both bf16: scale = (largest - least) / 15, and a channel
+ *   is code 0..15 = round((x - least) / scale) (half to even, clamped; exact in that no other arithmetic decides a rounding), which stands
+ *   for least + scale * code.  A group that holds a NaN or an infinity reads back as NaN.
+ * Supported: d = 32, 64 or 128, page_size a multiple of 16, max_pages * page_size <= 2^28, B * Hkv <= 32767.
+ */
+LOT_API size_t lot_cache4_bytes(int num_pages, int Hkv, int page_size, int d);
+
+/*
+ * lot_cache4_write -- tokens k, v [B,Hkv,m,d] of `dtype` go to positions start[b] .. start[b] + m - 1 of their sequences; with
+ * count [B] int32 (or NULL: m) only the first count[b] of them.  Positions outside [0, max_pages * page_size): not written
+ * (LOT_DEV_PAGE).  Two tokens of one call must not share a place.
+ */
+LOT_API int lot_cache4_write(const void *k, const void *v, const int32_t *pages, const int32_t *start, const int32_t *count,
+                     int dtype, int B, int Hkv, int m, int d, int page_size, int max_pages, int num_pages,
+                     void *cache, int32_t *status, lot_stream_t stream);
+
+/* lot_cache4_read -- the reverse: k, v [B,Hkv,m,d] get what the codes stand for; rows from count[b] on are left as they were. */
+LOT_API int lot_cache4_read(const void *cache, const int32_t *pages, const int32_t *start, const int32_t *count,
+                    int dtype, int B, int Hkv, int m, int d, int page_size, int max_pages, int num_pages,
+                    void *k, void *v, int32_t *status, lot_stream_t stream);
+
+/*
+ * lot_cache4_attention -- window attention (right = 0) of the last nq tokens of every sequence over its cache: length [B] int32 counts the
+ * tokens of sequence b in the cache (values outside [0, max_pages * page_size] are clamped), and query i stands at position
+ * length[b] - nq + i.  q, out [B,H,nq,d], lse [B,H,nq] or NULL; left, sinks, scale as above.  Only pages with visible tokens are read.
+ */
+LOT_API size_t lot_cache4_attention_workspace_bytes(int dtype, int B, int H, int Hkv, int nq, int d, int page_size, int max_pages, int left, int sinks);
+LOT_API int lot_cache4_attention(const void *q, const void *cache, const int32_t *pages, const int32_t *length,
+                         int dtype, int B, int H, int Hkv, int nq, int d, int page_size, int max_pages, int num_pages,
+                         int left, int sinks, float scale,
+                         void *out, float *lse, int32_t *status,
+                         void *ws, size_t ws_bytes, lot_stream_t stream);
 
 /*
  * lot_device_status -- copy the device status word of workspace `ws` (as passed to

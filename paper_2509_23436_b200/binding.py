@@ -7,6 +7,7 @@ There is no fallback: if the library cannot be loaded the first call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -15,7 +16,7 @@ import torch
 
 LOT_F32, LOT_BF16 = 0, 1
 LOT_OK = 0
-LOT_DEV_NONFINITE, LOT_DEV_EMPTY, LOT_DEV_TIMEOUT, LOT_DEV_RECOMPUTED, LOT_DEV_BOUNDS = 1, 2, 4, 8, 16
+LOT_DEV_NONFINITE, LOT_DEV_EMPTY, LOT_DEV_TIMEOUT, LOT_DEV_RECOMPUTED, LOT_DEV_BOUNDS, LOT_DEV_PAGE = 1, 2, 4, 8, 16, 32
 
 # LOT_LIBRARY selects another build of the same library (the bounds-check build liblot_debug.so)
 _LIB_PATH = os.environ.get("LOT_LIBRARY") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "liblot.so")
@@ -42,6 +43,15 @@ SIGNATURES = {
     "lot_attention_fwd": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _f, _i, _vp, _vp]),
     "lot_bwd_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
     "lot_attention_bwd": (_i, [_vp] * 7 + [_i] * 6 + [_f, _i] + [_vp] * 6 + [_sz, _vp]),
+    "lot_window_fwd_workspace_bytes": (_sz, [_i] * 10),
+    "lot_window_fwd": (_i, [_vp] * 5 + [_i] * 10 + [_f] + [_vp] * 4 + [_sz, _vp]),
+    "lot_window_bwd_workspace_bytes": (_sz, [_i] * 10),
+    "lot_window_bwd": (_i, [_vp] * 8 + [_i] * 10 + [_f] + [_vp] * 5 + [_sz, _vp]),
+    "lot_cache4_bytes": (_sz, [_i] * 4),
+    "lot_cache4_write": (_i, [_vp] * 5 + [_i] * 8 + [_vp] * 3),
+    "lot_cache4_read": (_i, [_vp] * 4 + [_i] * 8 + [_vp] * 4),
+    "lot_cache4_attention_workspace_bytes": (_sz, [_i] * 10),
+    "lot_cache4_attention": (_i, [_vp] * 4 + [_i] * 11 + [_f] + [_vp] * 4 + [_sz, _vp]),
     "lot_device_status": (_i, [_vp, _vp, ctypes.POINTER(_i)]),
 }
 
@@ -282,3 +292,170 @@ def lot_attention_bwd(q, k, v, z, beta, key_len, dout, eps, iters, *, ws=None, s
                                  _dev(dbeta, "dbeta", f32), _dev(ws, "ws"), ws.numel(), _stream(stream))
     _check(st, "lot_attention_bwd")
     return dq, dk, dv, dz, dbeta, ws
+
+
+def _band(q, k, v, key_len, q_start, left, right, sinks, scale):
+    """Sizes of a window attention call after its checks: (dtype code, B, H, Hkv, nq, nk, d, left, right, sinks, scale)."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise LotError("q must be [B,H,nq,d] and k, v [B,Hkv,nk,d]")
+    B, H, nq, d = q.shape
+    Hkv, nk = k.shape[1], k.shape[2]
+    if k.shape[0] != B or k.shape[3] != d or v.shape != k.shape or k.dtype is not q.dtype or v.dtype is not q.dtype:
+        raise LotError("k, v must be [B,Hkv,nk,d] in q's dtype")
+    for name, t in (("key_len", key_len), ("q_start", q_start)):
+        if t is not None and t.shape != (B,):
+            raise LotError(f"{name} must be [B]")
+    return (_dtype_code(q), B, H, Hkv, nq, nk, d, int(left), int(right), int(sinks), float(d ** -0.5 if scale is None else scale))
+
+
+def _same_device(first, **others):
+    for name, t in others.items():
+        if t is not None and t.device != first.device:
+            raise LotError(f"{name} is on {t.device}, the call's other tensors on {first.device}")
+
+
+def _guard(t: torch.Tensor):
+    """The tensors' device for the length of a call, when another one is current."""
+    if t.is_cuda and (_get_device is None or _get_device() != t.device.index):
+        return torch.cuda.device(t.device)
+    return contextlib.nullcontext()
+
+
+def lot_window_fwd(q, k, v, *, left, right=0, sinks=0, scale=None, key_len=None, q_start=None, out=None, lse=None, want_lse=False,
+                   status=None, ws=None, stream=None):
+    """Window attention with sinks.  scale None: d ** -0.5.  Returns (out, lse or None, ws or None)."""
+    sizes = _band(q, k, v, key_len, q_start, left, right, sinks, scale)
+    _same_device(q, k=k, v=v, key_len=key_len, q_start=q_start, out=out, lse=lse, status=status, ws=ws)
+    with _guard(q):
+        if out is None:
+            out = torch.empty_like(q)
+        elif out.shape != q.shape:
+            raise LotError("out must have q's shape")
+        if lse is None and want_lse:
+            lse = torch.empty(q.shape[:3], device=q.device, dtype=torch.float32)
+        elif lse is not None and lse.shape != q.shape[:3]:
+            raise LotError("lse must be [B,H,nq]")
+        if ws is None:
+            need = lib().lot_window_fwd_workspace_bytes(*sizes[:10])
+            ws = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
+        i32, f32 = torch.int32, torch.float32
+        st = lib().lot_window_fwd(_dev(q, "q"), _dev(k, "k"), _dev(v, "v"), _dev(key_len, "key_len", i32), _dev(q_start, "q_start", i32), *sizes,
+                                  _dev(out, "out", q.dtype), _dev(lse, "lse", f32), _dev(status, "status", i32), _dev(ws, "ws"),
+                                  0 if ws is None else ws.numel(), _stream(stream))
+    _check(st, "lot_window_fwd")
+    return out, lse, ws
+
+
+def lot_window_bwd(q, k, v, out, lse, dout, *, left, right=0, sinks=0, scale=None, key_len=None, q_start=None, dq=None, dk=None, dv=None,
+                   status=None, ws=None, stream=None):
+    """Gradients of lot_window_fwd with respect to q, k, v.  Returns (dq, dk, dv, ws or None)."""
+    sizes = _band(q, k, v, key_len, q_start, left, right, sinks, scale)
+    _same_device(q, k=k, v=v, out=out, lse=lse, dout=dout, key_len=key_len, q_start=q_start, dq=dq, dk=dk, dv=dv, status=status, ws=ws)
+    for name, t, like in (("out", out, q), ("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
+        if t is not None and t.shape != like.shape:
+            raise LotError(f"{name} must be {tuple(like.shape)}")
+    if lse.shape != q.shape[:3]:
+        raise LotError("lse must be [B,H,nq]")
+    with _guard(q):
+        dq = torch.empty_like(q) if dq is None else dq
+        dk = torch.empty_like(k) if dk is None else dk
+        dv = torch.empty_like(v) if dv is None else dv
+        if ws is None:
+            need = lib().lot_window_bwd_workspace_bytes(*sizes[:10])
+            ws = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
+        i32, dt = torch.int32, q.dtype
+        st = lib().lot_window_bwd(_dev(q, "q"), _dev(k, "k"), _dev(v, "v"), _dev(out, "out", dt), _dev(lse, "lse", torch.float32), _dev(dout, "dout", dt),
+                                  _dev(key_len, "key_len", i32), _dev(q_start, "q_start", i32), *sizes, _dev(dq, "dq", dt), _dev(dk, "dk", dt),
+                                  _dev(dv, "dv", dt), _dev(status, "status", i32), _dev(ws, "ws"), 0 if ws is None else ws.numel(), _stream(stream))
+    _check(st, "lot_window_bwd")
+    return dq, dk, dv, ws
+
+
+def lot_cache4_bytes(num_pages, Hkv, page_size, d) -> int:
+    return lib().lot_cache4_bytes(num_pages, Hkv, page_size, d)
+
+
+def lot_cache4_empty(num_pages, Hkv, page_size, d, device) -> torch.Tensor:
+    """A cache of zeros: [num_pages, Hkv, 2, page_size * (d/2 + d/8)] bytes."""
+    if lot_cache4_bytes(num_pages, Hkv, page_size, d) == 0:
+        raise LotError("lot_cache4_empty: unsupported sizes")
+    return torch.zeros(num_pages, Hkv, 2, page_size * (d // 2 + d // 8), device=device, dtype=torch.uint8)
+
+
+def _cache4(cache, pages, d, Hkv, **rows):
+    """(page_size, max_pages, num_pages) of a cache after its checks; rows: [B] tensors."""
+    if cache.dim() != 4 or cache.shape[2] != 2 or cache.shape[1] != Hkv or pages.dim() != 2:
+        raise LotError("cache must be [num_pages,Hkv,2,page_size*(d/2+d/8)] and pages [B,max_pages]")
+    per = d // 2 + d // 8
+    if per == 0 or cache.shape[3] % per:
+        raise LotError(f"cache rows do not fit d = {d}")
+    for name, t in rows.items():
+        if t is not None and t.shape != (pages.shape[0],):
+            raise LotError(f"{name} must be [B]")
+    return cache.shape[3] // per, pages.shape[1], cache.shape[0]
+
+
+def lot_cache4_write(cache, pages, k, v, start, *, count=None, status=None, stream=None):
+    """Tokens k, v [B,Hkv,m,d] into the cache at positions start[b] and on.  Returns cache."""
+    if k.dim() != 4 or v.shape != k.shape or v.dtype is not k.dtype:
+        raise LotError("k, v must be [B,Hkv,m,d] of one dtype")
+    B, Hkv, m, d = k.shape
+    sizes = _cache4(cache, pages, d, Hkv, start=start, count=count)
+    if pages.shape[0] != B:
+        raise LotError("pages must be [B,max_pages]")
+    _same_device(k, v=v, cache=cache, pages=pages, start=start, count=count, status=status)
+    i32 = torch.int32
+    with _guard(k):
+        st = lib().lot_cache4_write(_dev(k, "k"), _dev(v, "v"), _dev(pages, "pages", i32), _dev(start, "start", i32), _dev(count, "count", i32),
+                                    _dtype_code(k), B, Hkv, m, d, *sizes, _dev(cache, "cache", torch.uint8), _dev(status, "status", i32), _stream(stream))
+    _check(st, "lot_cache4_write")
+    return cache
+
+
+def lot_cache4_read(cache, pages, start, m, *, d, dtype=torch.bfloat16, count=None, k=None, v=None, status=None, stream=None):
+    """Tokens start[b] .. start[b] + m - 1 of every sequence as k, v [B,Hkv,m,d].  Returns (k, v)."""
+    B, Hkv = pages.shape[0], cache.shape[1]
+    sizes = _cache4(cache, pages, d, Hkv, start=start, count=count)
+    _same_device(cache, pages=pages, start=start, count=count, k=k, v=v, status=status)
+    i32 = torch.int32
+    with _guard(cache):
+        k = torch.empty(B, Hkv, m, d, device=cache.device, dtype=dtype) if k is None else k
+        v = torch.empty(B, Hkv, m, d, device=cache.device, dtype=dtype) if v is None else v
+        if k.shape != (B, Hkv, m, d) or v.shape != k.shape:
+            raise LotError("k, v must be [B,Hkv,m,d]")
+        st = lib().lot_cache4_read(_dev(cache, "cache", torch.uint8), _dev(pages, "pages", i32), _dev(start, "start", i32), _dev(count, "count", i32),
+                                   _dtype_code(k), B, Hkv, m, d, *sizes, _dev(k, "k"), _dev(v, "v", k.dtype), _dev(status, "status", i32), _stream(stream))
+    _check(st, "lot_cache4_read")
+    return k, v
+
+
+def lot_cache4_attention(q, cache, pages, length, *, left=-1, sinks=0, scale=None, out=None, lse=None, want_lse=False, status=None, ws=None,
+                         stream=None):
+    """Attention of the last nq tokens of every sequence over its cache.  Returns (out, lse or None, ws or None)."""
+    if q.dim() != 4:
+        raise LotError("q must be [B,H,nq,d]")
+    B, H, nq, d = q.shape
+    Hkv = cache.shape[1]
+    page_size, max_pages, num_pages = _cache4(cache, pages, d, Hkv, length=length)
+    if pages.shape[0] != B:
+        raise LotError("pages must be [B,max_pages]")
+    _same_device(q, cache=cache, pages=pages, length=length, out=out, lse=lse, status=status, ws=ws)
+    code, i32 = _dtype_code(q), torch.int32
+    with _guard(q):
+        if out is None:
+            out = torch.empty_like(q)
+        elif out.shape != q.shape:
+            raise LotError("out must have q's shape")
+        if lse is None and want_lse:
+            lse = torch.empty(q.shape[:3], device=q.device, dtype=torch.float32)
+        elif lse is not None and lse.shape != q.shape[:3]:
+            raise LotError("lse must be [B,H,nq]")
+        if ws is None:
+            need = lib().lot_cache4_attention_workspace_bytes(code, B, H, Hkv, nq, d, page_size, max_pages, int(left), int(sinks))
+            ws = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
+        st = lib().lot_cache4_attention(_dev(q, "q"), _dev(cache, "cache", torch.uint8), _dev(pages, "pages", i32), _dev(length, "length", i32),
+                                        code, B, H, Hkv, nq, d, page_size, max_pages, num_pages, int(left), int(sinks),
+                                        float(d ** -0.5 if scale is None else scale), _dev(out, "out", q.dtype), _dev(lse, "lse", torch.float32),
+                                        _dev(status, "status", i32), _dev(ws, "ws"), 0 if ws is None else ws.numel(), _stream(stream))
+    _check(st, "lot_cache4_attention")
+    return out, lse, ws

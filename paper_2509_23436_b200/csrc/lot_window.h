@@ -1,0 +1,69 @@
+// Internal launch interface of window attention (lot_window_fwd, lot_window_bwd) and of the 4-bit cache.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace lot {
+namespace window {
+
+constexpr int kFar = 1 << 30;              // left, right without limit: positions stay below 2^29, sums inside 32 bits
+constexpr int kMaxPos = 1 << 29;
+
+struct Band {                              // which keys a query sees
+    const int32_t *key_len;                // [B] or nullptr (nk)
+    const int32_t *q_start;                // [B] or nullptr (nk - nq)
+    int nq, nk, left, right, sinks;        // left, right <= kFar, sinks <= nk
+};
+
+struct Fwd {
+    Band band;
+    const void *q, *k, *v;                 // [B][H][nq][d], [B][Hkv][nk][d]
+    void *out;                             // [B][H][nq][d]
+    float *lse;                            // [B][H][nq] or nullptr
+    int dtype, B, H, Hkv, d;
+    float scale;
+    int *status;                           // or nullptr
+};
+
+struct Bwd {
+    Band band;
+    const void *q, *k, *v, *out, *dout;
+    const float *lse;
+    void *dq, *dk, *dv;
+    float *delta;                          // [B][H][nq] scratch: <dout, out> of every row
+    int dtype, B, H, Hkv, d;
+    float scale;
+    int *status;
+};
+
+struct Cache4 {                            // [num_pages][Hkv][2][page_size * (d/2 + d/8)] bytes
+    uint8_t *base;
+    const int32_t *pages;                  // [B][max_pages]
+    int num_pages, max_pages, page_size, Hkv, d;
+};
+
+struct Attend4 {
+    Cache4 cache;
+    Band band;                             // key_len = length, nk = capacity of the page table, q_start unused (length - nq)
+    const void *q;
+    void *out;
+    float *lse;
+    int dtype, B, H;
+    float scale;
+    int *status;
+    void *ws;                              // attend4_workspace bytes
+};
+
+cudaError_t launch_fwd(const Fwd &a, cudaStream_t st);
+cudaError_t launch_bwd(const Bwd &a, cudaStream_t st);
+size_t attend4_workspace(int dtype, int B, int H, int Hkv, int nq, int d, int nk, int left, int sinks);
+cudaError_t launch_attend4(const Attend4 &a, cudaStream_t st);
+cudaError_t launch_write4(const Cache4 &c, const void *k, const void *v, const int32_t *start, const int32_t *count, int dtype, int B, int m, int *status,
+                          cudaStream_t st);
+cudaError_t launch_read4(const Cache4 &c, void *k, void *v, const int32_t *start, const int32_t *count, int dtype, int B, int m, int *status,
+                         cudaStream_t st);
+
+} // namespace window
+} // namespace lot
