@@ -1,0 +1,407 @@
+// Window attention forward of bf16 tensors on tcgen05.
+//
+// A persistent block per SM goes through items of two 128-query tiles that read the same keys: two query heads of a key head, or two
+// neighbouring tiles of one head.  Five roles: two groups of four softmax warps (one a query tile, a thread a row), one warp that loads
+// tiles (TMA), one that issues the products.  For each 128-key tile
+//   S = Q K^T in tensor memory -> the group's rows: maximum, exponentials, sum -> P (bf16) back into tensor memory, where it is the first
+//   operand of O += P V -> O stays in tensor memory over the item's tiles.
+// The running maximum moves only when a score passes it by 2^8 (weights up to 2^8 lose nothing in float32 sums or bf16 weights), so O is
+// hardly ever rescaled.  While one group takes exponentials the products of the other run.
+// Key tiles outside a block's window are never visited, 32-column parts outside a warp's never worked on.
+#include "lot_chain.cuh"
+#include "lot_window_tc.cuh"
+
+#include <mutex>
+
+namespace lot {
+namespace window {
+namespace {
+
+constexpr int kThreads = 320, kMmaWarp = 8, kLoadWarp = 9;
+constexpr float kLift = 8.f;
+
+template <int DP> struct Plan {
+    static constexpr bool kApart = DP == 64;               // P has columns of its own: the next S may be written while P is made
+    static constexpr int kQStages = DP == 64 ? 2 : 1, kSlots = DP == 64 ? 8 : 4;
+    static constexpr int kQ = 0, kKV = kQStages * 2 * kTileBytes<DP>, kBars = kKV + kSlots * kTileBytes<DP>;
+    // q_full, q_empty [stages]; kv_full, kv_empty [slots]; s_full, s_free, p_full, o_done [2]
+    static constexpr int bQFull = kBars, bQEmpty = bQFull + 8 * kQStages, bFull = bQEmpty + 8 * kQStages, bEmpty = bFull + 8 * kSlots, bS = bEmpty + 8 * kSlots,
+                         bSFree = bS + 16, bP = bSFree + 16, bO = bP + 16, kAbort = bO + 16, kTmem = kAbort + 8, kTotal = kTmem + 8;
+    static constexpr int cS = 0, cP = kApart ? 128 : 0, cO = kApart ? 192 : 128, kCols = 256;      // columns of a tile's half of tensor memory
+};
+
+struct Args {
+    Fwd a;
+    CUtensorMap q, k, v;
+    int G, paired, tiles, per_tile, items;                 // paired: two heads of a key head; tiles: query tiles of a head
+};
+
+struct Item {
+    Row R;
+    int b, h0, row0, hk, hstep, rstep;                     // head and first query of the two tiles
+    KeyTiles keys;
+    __device__ __forceinline__ int head(int t) const { return h0 + (t ? hstep : 0); }
+    __device__ __forceinline__ int row(int t) const { return row0 + (t ? rstep : 0); }
+};
+__device__ __forceinline__ Item item_of(const Args &A, int i)
+{
+    Item it;
+    // last query tiles first: with a window that is not limited to the left they are the longest
+    const int per = A.per_tile, t = (A.paired ? A.tiles : (A.tiles + 1) / 2) - 1 - i / per, x = i % per, heads = A.paired ? A.a.H / 2 : A.a.H;
+    it.b = x / heads;
+    const int y = x % heads;
+    it.h0 = A.paired ? 2 * y : y;
+    it.hstep = A.paired ? 1 : 0;
+    it.row0 = A.paired ? t * kTile : 2 * t * kTile;
+    it.rstep = A.paired ? 0 : kTile;
+    it.hk = it.h0 / A.G;
+    it.R = row_of(A.a.band, it.b);
+    it.keys = key_tiles(it.R, it.R.pos + it.row0, it.R.pos + min(it.row0 + it.rstep + kTile, A.a.band.nq) - 1);
+    return it;
+}
+// The key tiles of all items of this block, one after the other; items that see nothing have none.
+struct Walk {
+    Item it;
+    int i, tile, count;                                    // count: items with tiles so far
+    __device__ __forceinline__ void begin(const Args &A)
+    {
+        i = blockIdx.x;
+        tile = 0;
+        count = 0;
+        settle_on(A);
+    }
+    __device__ __forceinline__ void settle_on(const Args &A)
+    {
+        while (i < A.items) {
+            it = item_of(A, i);
+            if (it.keys.n > 0) return;
+            i += gridDim.x;
+        }
+    }
+    __device__ __forceinline__ bool more(const Args &A) const { return i < A.items; }
+    __device__ __forceinline__ void next(const Args &A)
+    {
+        if (++tile < it.keys.n) return;
+        tile = 0;
+        ++count;
+        i += gridDim.x;
+        settle_on(A);
+    }
+};
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_constant__ Args A)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    using P = Plan<DP>;
+    constexpr int TB = kTileBytes<DP>;
+    const uint32_t sbase = smem_u32(smem);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + P::kAbort);
+    const Waits wait{abort_flag, A.a.status != nullptr ? A.a.status : reinterpret_cast<int *>(smem + P::kAbort + 4)};
+    if (tid == 0) {
+        for (int s = 0; s < P::kQStages; ++s) { mbar_init(sbase + P::bQFull + 8 * s, 1); mbar_init(sbase + P::bQEmpty + 8 * s, 1); }
+        for (int s = 0; s < P::kSlots; ++s) { mbar_init(sbase + P::bFull + 8 * s, 1); mbar_init(sbase + P::bEmpty + 8 * s, 1); }
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(sbase + P::bS + 8 * t, 1);
+            mbar_init(sbase + P::bSFree + 8 * t, 4);
+            mbar_init(sbase + P::bP + 8 * t, 4);
+            mbar_init(sbase + P::bO + 8 * t, 1);
+        }
+        abort_flag[0] = abort_flag[1] = 0;
+        fence_barrier_init();
+    }
+    if (warp == kMmaWarp) { tmem_alloc(sbase + P::kTmem, 512); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(smem + P::kTmem);
+
+    if (warp == kLoadWarp) {
+        Walk w;
+        uint32_t n = 0;                                    // tiles loaded, keys and values counted apart
+        bool ok = true;
+        for (w.begin(A); ok && w.more(A); w.next(A)) {
+            const int j0 = w.it.keys.at(w.tile) * kTile, kv = w.it.b * A.a.Hkv + w.it.hk;
+            if (w.tile == 0) {
+                const int s = w.count % P::kQStages;
+                const uint32_t turn = w.count / P::kQStages;
+                if (turn > 0 && !wait(sbase + P::bQEmpty + 8 * s, turn - 1)) break;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(sbase + P::bQFull + 8 * s, 2 * TB);
+                    for (int t = 0; t < 2; ++t)
+                        load_tile<DP>(sbase + P::kQ + (2 * s + t) * TB, &A.q, sbase + P::bQFull + 8 * s, w.it.row(t), w.it.b * A.a.H + w.it.head(t));
+                }
+                __syncwarp();
+            }
+            for (int side = 0; ok && side < 2; ++side, ++n) {
+                const uint32_t s = n % P::kSlots, turn = n / P::kSlots;
+                if (turn > 0 && !wait(sbase + P::bEmpty + 8 * s, turn - 1)) { ok = false; break; }
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(sbase + P::bFull + 8 * s, TB);
+                    load_tile<DP>(sbase + P::kKV + s * TB, side ? &A.v : &A.k, sbase + P::bFull + 8 * s, j0, kv);
+                }
+                __syncwarp();
+            }
+        }
+        if (*abort_flag) {                                 // copies still on their way land before the block ends
+            for (uint32_t u = n > P::kSlots ? n - P::kSlots : 0; u < n; ++u)
+                for (int x = 0; x < 4096 && !mbar_try_wait(sbase + P::bFull + 8 * (u % P::kSlots), (u / P::kSlots) & 1); ++x) {}
+        }
+    } else if (warp == kMmaWarp) {
+        Walk w, ahead;
+        w.begin(A);
+        ahead = w;
+        uint32_t g = 0;                                    // tiles done
+        bool ok = true;
+        // S of the tile `ahead` stands at, its place among this block's tiles `at`
+        auto scores = [&](uint32_t at, int t) {
+            if (elect_one()) {
+                product_rows<DP>(tmem + t * P::kCols + P::cS, sbase + P::kQ + (2 * (ahead.count % P::kQStages) + t) * TB, sbase + P::kKV + (2 * at % P::kSlots) * TB);
+                umma_commit(sbase + P::bS + 8 * t);
+                if (t == 1) {
+                    umma_commit(sbase + P::bEmpty + 8 * (2 * at % P::kSlots));
+                    if (ahead.tile == ahead.it.keys.n - 1) umma_commit(sbase + P::bQEmpty + 8 * (ahead.count % P::kQStages));
+                }
+            }
+            __syncwarp();
+        };
+        auto operands = [&](uint32_t at) {                 // its queries and keys have come
+            if (ahead.tile == 0 && !wait(sbase + P::bQFull + 8 * (ahead.count % P::kQStages), ahead.count / P::kQStages)) return false;
+            return wait(sbase + P::bFull + 8 * (2 * at % P::kSlots), 2 * at / P::kSlots);
+        };
+        if (w.more(A)) {
+            ok = operands(0);
+            if (ok) { scores(0, 0); scores(0, 1); ahead.next(A); }
+        }
+        for (; ok && w.more(A); w.next(A), ++g) {
+            const bool follow = ahead.more(A);
+            const uint32_t vs = (2 * g + 1) % P::kSlots;
+            if (P::kApart && follow) {
+                ok = operands(g + 1);
+                for (int t = 0; ok && t < 2; ++t) {
+                    ok = wait(sbase + P::bSFree + 8 * t, g);
+                    if (!ok) break;
+                    tc_fence_after();
+                    scores(g + 1, t);
+                }
+                if (!ok) break;
+            }
+            ok = wait(sbase + P::bFull + 8 * vs, (2 * g + 1) / P::kSlots);
+            if (!ok) break;
+            const int j0 = w.it.keys.at(w.tile) * kTile;
+            if (!all_used(w.it.R, j0)) clear_unused<DP>(smem + P::kKV + vs * TB, w.it.R, j0, lane);
+            for (int t = 0; t < 2; ++t) {
+                ok = wait(sbase + P::bP + 8 * t, g);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    product_weights<DP>(tmem + t * P::kCols + P::cO, tmem + t * P::kCols + P::cP, sbase + P::kKV + vs * TB, w.tile > 0);
+                    umma_commit(sbase + P::bO + 8 * t);
+                    if (t == 1) umma_commit(sbase + P::bEmpty + 8 * vs);
+                }
+                __syncwarp();
+                if (!P::kApart && follow) {
+                    if (t == 0) ok = operands(g + 1);
+                    if (!ok) break;
+                    scores(g + 1, t);
+                }
+            }
+            if (follow) ahead.next(A);
+        }
+        if (*abort_flag) {                                 // products on their way end before tensor memory is given back
+            for (int x = 0; x < 4096; ++x) (void)mbar_try_wait(sbase + P::bO, (g & 1) ^ 1);
+        }
+    } else {
+        const int t = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * P::kCols;
+        const float c = A.a.scale * kLog2e;
+        uint32_t g = 0;
+        bool ok = true;
+        for (int i = blockIdx.x; i < A.items; i += gridDim.x) {
+            const Item it = item_of(A, i);
+            const Row &R = it.R;
+            const int q = it.row(t) + row, p = R.pos + q, pw0 = R.pos + it.row(t) + (warp & 3) * 32, pw1 = pw0 + 31;
+            float m = neg_inf(), l = 0.f;
+            for (int n = 0; ok && n < it.keys.n; ++n, ++g) {
+                const int j0 = it.keys.at(n) * kTile;
+                float s[2][32];                            // S is read twice, 32 columns at a time, the next ones on their way
+                int kind[4];                               // of 32 columns, for the warp: 0 nothing seen, 1 a part, 2 all
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int a = j0 + 32 * k, b = a + 31;
+                    kind[k] = a > R.hi(pw1) || (b < pw0 - R.left && a >= R.sinks) ? 0 : b <= R.hi(pw0) && (a >= pw1 - R.left || b < R.sinks) ? 2 : 1;
+                }
+                ok = wait(sbase + P::bS + 8 * t, g);
+                if (!ok) break;
+                tc_fence_after();
+                float top = neg_inf();
+                tmem_ld32(lanes + P::cS, s[0]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float (&x)[32] = s[k & 1];
+                    settle(x);
+                    tmem_ld32(lanes + P::cS + 32 * ((k + 1) & 3), s[(k + 1) & 1]);
+                    if (kind[k] == 0) continue;
+                    if (kind[k] == 1) {
+                        const uint32_t seen = seen_keys(R, p, j0 + 32 * k);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[e] = (seen >> e) & 1u ? x[e] : neg_inf();
+                    }
+                    float y[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                    for (int e = 4; e < 32; ++e) y[e & 3] = fmaxf(y[e & 3], x[e]);
+                    top = fmaxf(top, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+                }
+                top *= c;
+                const bool lift = __any_sync(0xffffffffu, top > m + kLift);
+                float f = 1.f;
+                if (lift) {
+                    const float to = fmaxf(m, top);
+                    f = to == neg_inf() ? 1.f : ex2(m - to);
+                    l *= f;
+                    m = to;
+                }
+                const float ref = m == neg_inf() ? 0.f : m;
+                if (g > 0) {                               // P is free, O may be touched
+                    ok = wait(sbase + P::bO + 8 * t, g - 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                if (lift && n > 0) {
+                    settle(s[0]);
+#pragma unroll
+                    for (int k = 0; k < DP / 32; ++k) {
+                        tmem_ld32(lanes + P::cO + 32 * k, s[1]);
+                        settle(s[1]);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) s[1][e] *= f;
+                        tmem_st32(lanes + P::cO + 32 * k, reinterpret_cast<const uint32_t *>(s[1]));
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float (&x)[32] = s[k & 1];
+                    settle(x);
+                    if (k < 3) tmem_ld32(lanes + P::cS + 32 * (k + 1), s[(k + 1) & 1]);
+                    else if (P::kApart) {                  // all of S has been read
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(sbase + P::bSFree + 8 * t);
+                    }
+                    uint32_t w[16];
+                    if (kind[k] == 0) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[e] = 0u;
+                    } else {
+                        if (kind[k] == 1) {
+                            const uint32_t seen = seen_keys(R, p, j0 + 32 * k);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] = (seen >> e) & 1u ? x[e] : neg_inf();
+                        }
+                        float sum[2] = {0.f, 0.f};
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            x[e] = ex2(fmaf(x[e], c, -ref));
+                            sum[e & 1] += x[e];
+                        }
+                        l += sum[0] + sum[1];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[e] = tile::pack_bf16(x[2 * e], x[2 * e + 1]);
+                    }
+                    tmem_st16(lanes + P::cP + 16 * k, w);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sbase + P::bP + 8 * t);
+            }
+            if (ok && it.keys.n > 0) {
+                ok = wait(sbase + P::bO + 8 * t, g - 1);
+                tc_fence_after();
+            }
+            const float inv = !ok ? __int_as_float(0x7fc00000) : l > 0.f ? 1.f / l : 0.f;
+            const bool there = q < A.a.band.nq;
+            const size_t at = ((size_t)it.b * A.a.H + it.head(t)) * A.a.band.nq + q;
+#pragma unroll
+            for (int k = 0; k < DP / 32; ++k) {
+                float o[32];
+                if (it.keys.n > 0) {
+                    tmem_ld32(lanes + P::cO + 32 * k, o);
+                    settle(o);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                }
+                // a row that sees nothing: its sums are zero
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] *= inv;
+                if (there) store_row32(static_cast<__nv_bfloat16 *>(A.a.out) + at * A.a.d, 32 * k, A.a.d, o);
+            }
+            if (there && A.a.lse != nullptr) A.a.lse[at] = !ok ? inv : l > 0.f ? m * kLn2 + logf(l) : neg_inf();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+}
+
+template <int DP> cudaError_t launch_t(const Args &A, cudaStream_t st)
+{
+    static std::mutex mu;
+    static bool set[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!set[dev]) {
+            const cudaError_t e = cudaFuncSetAttribute(fwd_tc_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<DP>::kTotal);
+            if (e != cudaSuccess) return e;
+            set[dev] = true;
+        }
+    }
+    const int sms = device_sm_count();
+    fwd_tc_kernel<DP><<<A.items < sms ? A.items : sms, kThreads, Plan<DP>::kTotal, st>>>(A);
+    return cudaGetLastError();
+}
+
+} // namespace
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+bool make_tile_map(CUtensorMap *m, const void *base, long long outer, int rows, int cols)
+{
+    static EncodeTiledFn fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) == cudaSuccess && found == cudaDriverEntryPointSuccess
+                   ? reinterpret_cast<EncodeTiledFn>(p) : nullptr;
+    }();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)outer}, strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)rows * cols * 2};
+    const cuuint32_t box[3] = {64u, (cuuint32_t)kTile, 1u}, es[3] = {1u, 1u, 1u};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t launch_fwd_tc(const Fwd &a, cudaStream_t st)
+{
+    Args A;
+    A.a = a;
+    A.G = a.H / a.Hkv;
+    A.paired = A.G % 2 == 0;
+    A.tiles = (a.band.nq + kTile - 1) / kTile;
+    A.per_tile = a.B * (A.paired ? a.H / 2 : a.H);
+    A.items = (A.paired ? A.tiles : (A.tiles + 1) / 2) * A.per_tile;
+    if (!make_tile_map(&A.q, a.q, (long long)a.B * a.H, a.band.nq, a.d)) return cudaErrorInvalidValue;
+    A.k = A.v = A.q;                                       // without keys no item has tiles
+    if (a.band.nk > 0 && (!make_tile_map(&A.k, a.k, (long long)a.B * a.Hkv, a.band.nk, a.d) ||
+                          !make_tile_map(&A.v, a.v, (long long)a.B * a.Hkv, a.band.nk, a.d)))
+        return cudaErrorInvalidValue;
+    return a.d <= 64 ? launch_t<64>(A, st) : launch_t<128>(A, st);
+}
+
+} // namespace window
+} // namespace lot

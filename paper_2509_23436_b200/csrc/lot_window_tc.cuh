@@ -1,0 +1,154 @@
+// What the tcgen05 kernels of window attention share: tiles of 128 rows in shared memory, key tiles a block of queries sees, masks of 32
+// columns, products with the first operand in tensor memory.
+#pragma once
+
+#include "lot_sm100.cuh"
+#include "lot_tile.cuh"
+#include "lot_window.cuh"
+
+namespace lot {
+int device_sm_count();
+namespace window {
+
+using namespace sm100;
+
+constexpr int kTile = 128;
+
+// Key tiles that queries at positions p0 .. p1 see: those of the sinks below the window's first, then the window's.
+struct KeyTiles {
+    int sink, first, n;                    // tiles 0 .. sink - 1, then first ..; n in all
+    __device__ __forceinline__ int at(int i) const { return i < sink ? i : first + i - sink; }
+};
+__device__ __forceinline__ KeyTiles key_tiles(const Row &R, int p0, int p1)
+{
+    KeyTiles t;
+    const int hi = R.hi(p1), last = hi < 0 ? -1 : hi / kTile;
+    t.first = R.lo(p0) / kTile;
+    t.sink = max(min((min(R.sinks, hi + 1) + kTile - 1) / kTile, t.first), 0);
+    t.n = t.sink + max(last - t.first + 1, 0);
+    return t;
+}
+
+__device__ __forceinline__ uint32_t bits_between(int a, int b)      // bits a .. b (clamped to 0 .. 31)
+{
+    a = max(a, 0);
+    b = min(b, 31);
+    return a > b ? 0u : (0xffffffffu >> (31 - b)) & (0xffffffffu << a);
+}
+// which of the keys j .. j + 31 the query at p sees
+__device__ __forceinline__ uint32_t seen_keys(const Row &R, int p, int j)
+{
+    const int hi = R.hi(p) - j;
+    return bits_between(p - R.left - j, hi) | bits_between(0, min(hi, R.sinks - 1 - j));
+}
+// which of the queries at positions p .. p + 31 see key j
+__device__ __forceinline__ uint32_t seeing(const Row &R, int p, int j)
+{
+    if (j >= R.len) return 0u;
+    return bits_between(j - R.right - p, j < R.sinks ? 31 : j + R.left - p);
+}
+
+// ---- shared memory: a tile is DP / 64 panels of 128 rows x 128 bytes, 16-byte chunks permuted by the row (128-byte swizzle) ----
+template <int DP> constexpr int kTileBytes = kTile * DP * 2;
+
+template <int DP> __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int row, int outer)
+{
+#pragma unroll
+    for (int p = 0; p < DP / 64; ++p) tma_load_3d(dst + p * kTile * 128, map, bar, p * 64, row, outer);
+}
+// rows of a tile of keys or values that no query sees: whatever they hold, zeros take part in the products (whole warp)
+template <int DP> __device__ __forceinline__ void clear_unused(uint8_t *tile, const Row &R, int j0, int lane)
+{
+    for (int r = lane; r < kTile; r += 32) {
+        if (R.used(j0 + r)) continue;
+#pragma unroll
+        for (int p = 0; p < DP / 64; ++p) {
+            uint4 *x = reinterpret_cast<uint4 *>(tile + p * kTile * 128 + r * 128);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) x[c] = make_uint4(0, 0, 0, 0);
+        }
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+__device__ __forceinline__ bool all_used(const Row &R, int j0) { return R.used(j0) && j0 + kTile <= R.len && (j0 >= R.first || j0 + kTile <= R.sinks); }
+
+// ---- products, issued by one thread -----------------------------------------------------------------------------------
+// D (tensor memory, 128 x N) = or += A (tensor memory, 128 x 16 bf16: two to a column) B
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "setp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// D = X Y^T over DP channels, both tiles with 64 channels a panel row; N rows of Y
+template <int DP, int N = kTile> __device__ __forceinline__ void product_rows(uint32_t d, uint32_t x, uint32_t y)
+{
+    constexpr uint32_t idesc = make_idesc_bf16(128, N, 0, 0);
+    const uint64_t dx = make_smem_desc(x, 16, 1024), dy = make_smem_desc(y, 16, 1024);
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ++ks) {
+        const uint32_t off = (ks >> 2) * (kTile * 128 / 16) + (ks & 3) * 2;
+        umma_bf16(d, dx + off, dy + off, idesc, ks != 0);
+    }
+}
+// D (128 x DP) += W Y: W 128 x 128 bf16 in tensor memory, Y's 128 rows
+template <int DP> __device__ __forceinline__ void product_weights(uint32_t d, uint32_t w, uint32_t y, bool accumulate)
+{
+    constexpr uint32_t idesc = make_idesc_bf16(128, DP, 0, 1);
+    const uint64_t dy = make_smem_desc(y, kTile * 128, 1024);
+#pragma unroll
+    for (int ks = 0; ks < kTile / 16; ++ks) umma_bf16_ts(d, w + ks * 8, dy + ks * 128, idesc, accumulate || ks != 0);
+}
+
+// ---- tensor memory ------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// Behind it the 32 columns just requested may be used.
+__device__ __forceinline__ void settle(float (&v)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]),
+                   "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15])::"memory");
+    asm volatile("" : "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]),
+                   "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])::"memory");
+}
+
+// 32 numbers of one row as bf16 to columns col .. col + 31 of a [rows][d] tensor; d is a multiple of 8
+__device__ __forceinline__ void store_row32(__nv_bfloat16 *row, int col, int d, const float (&v)[32])
+{
+#pragma unroll
+    for (int c = 0; c < 32; c += 8)
+        if (col + c < d)
+            *reinterpret_cast<uint4 *>(row + col + c) = make_uint4(tile::pack_bf16(v[c], v[c + 1]), tile::pack_bf16(v[c + 2], v[c + 3]),
+                                                                    tile::pack_bf16(v[c + 4], v[c + 5]), tile::pack_bf16(v[c + 6], v[c + 7]));
+}
+
+// ---- barriers -------------------------------------------------------------------------------------------------------------
+struct Waits {                             // bounded waits of one block: the first that gives up ends them all
+    volatile int *abort_flag;
+    int *status;
+    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t phase) const { return mbar_wait(bar, phase & 1u, abort_flag, status); }
+};
+
+// host: bf16 tensor [outer][rows][cols], box 64 columns x 128 rows; columns and rows beyond the tensor read as zeros
+bool make_tile_map(CUtensorMap *m, const void *base, long long outer, int rows, int cols);
+
+} // namespace window
+} // namespace lot
