@@ -374,7 +374,7 @@ cudaError_t launch_fwd(const Fwd &a, cudaStream_t st)
 cudaError_t launch_bwd(const Bwd &a, cudaStream_t st)
 {
     if (a.dtype == 0) return a.d <= 32 ? bwd_t<float, 32>(a, st) : a.d <= 64 ? bwd_t<float, 64>(a, st) : bwd_t<float, 128>(a, st);
-    return a.d <= 32 ? bwd_t<__nv_bfloat16, 32>(a, st) : a.d <= 64 ? bwd_t<__nv_bfloat16, 64>(a, st) : bwd_t<__nv_bfloat16, 128>(a, st);
+    return launch_bwd_tc(a, st);
 }
 
 } // namespace window

@@ -32,7 +32,7 @@ struct Bwd {
     const void *q, *k, *v, *out, *dout;
     const float *lse;
     void *dq, *dk, *dv;
-    float *delta;                          // [B][H][nq] scratch: <dout, out> of every row
+    float *delta;                          // the workspace: <dout, out> of every row, and what bf16 tensors need besides
     int dtype, B, H, Hkv, d;
     float scale;
     int *status;
@@ -59,6 +59,8 @@ struct Attend4 {
 cudaError_t launch_fwd(const Fwd &a, cudaStream_t st);
 cudaError_t launch_fwd_tc(const Fwd &a, cudaStream_t st);      // bf16 tensors (lot_window_tc.cu)
 cudaError_t launch_bwd(const Bwd &a, cudaStream_t st);
+cudaError_t launch_bwd_tc(const Bwd &a, cudaStream_t st);      // bf16 tensors (lot_window_tc_bwd.cu)
+size_t bwd_tc_workspace(int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks);
 size_t attend4_workspace(int dtype, int B, int H, int Hkv, int nq, int d, int nk, int left, int sinks);
 cudaError_t launch_attend4(const Attend4 &a, cudaStream_t st);
 cudaError_t launch_write4(const Cache4 &c, const void *k, const void *v, const int32_t *start, const int32_t *count, int dtype, int B, int m, int *status,

@@ -67,9 +67,10 @@ int lot_window_fwd(const void *q, const void *k, const void *v, const int32_t *k
 
 size_t lot_window_bwd_workspace_bytes(int dtype, int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks)
 {
-    (void)left; (void)right;
-    if (check_sizes(dtype, B, H, Hkv, nq, nk, d, sinks) != LOT_OK) return 0;
-    return up256((size_t)B * H * nq * 4);
+    if (check_sizes(dtype, B, H, Hkv, nq, nk, d, sinks) != LOT_OK || B == 0) return 0;
+    if (dtype == LOT_F32) return up256((size_t)B * H * nq * 4);
+    const Band b = band_of(nullptr, nullptr, nq, nk, left, right, sinks);
+    return bwd_tc_workspace(B, H, Hkv, nq, nk, d, b.left, b.right, b.sinks);
 }
 
 int lot_window_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *dout,
