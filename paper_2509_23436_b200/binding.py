@@ -7,7 +7,6 @@ There is no fallback: if the library cannot be loaded the first call raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -308,40 +307,61 @@ def _band(q, k, v, key_len, q_start, left, right, sinks, scale):
     return (_dtype_code(q), B, H, Hkv, nq, nk, d, int(left), int(right), int(sinks), float(d ** -0.5 if scale is None else scale))
 
 
-def _same_device(first, **others):
-    for name, t in others.items():
-        if t is not None and t.device != first.device:
-            raise LotError(f"{name} is on {t.device}, the call's other tensors on {first.device}")
+# As above, one expression a tensor: the pointer of a contiguous tensor of the type on device `index`, or None.
+def _ptr(t: Optional[torch.Tensor], name: str, dtype, index: int):
+    if t is None:
+        return None
+    if not (t.dtype is dtype and t.is_contiguous() and t.get_device() == index and index >= 0):
+        if t.is_cuda and index >= 0 and t.get_device() != index:
+            raise LotError(f"{name} is on cuda:{t.get_device()}, the call's first tensor on cuda:{index}")
+        _refuse(t, name, dtype)
+    return t.data_ptr()
 
 
-def _guard(t: torch.Tensor):
-    """The tensors' device for the length of a call, when another one is current."""
-    if t.is_cuda and (_get_device is None or _get_device() != t.device.index):
-        return torch.cuda.device(t.device)
-    return contextlib.nullcontext()
+def _call(fn, index: int, args):
+    """fn(*args) with the tensors' device current."""
+    if _get_device is not None and _get_device() == index:
+        return fn(*args)
+    with torch.cuda.device(index):
+        return fn(*args)
+
+
+def _stream_of(stream, index: int) -> int:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(index)
+    if stream is None:
+        return torch.cuda.current_stream(index).cuda_stream
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _work(ws, need_fn, sizes, index):
+    """A workspace of the size the call asks for, when the caller brings none (the size may depend on the device)."""
+    if ws is not None:
+        return ws
+    need = _call(need_fn, index, sizes)
+    return torch.empty(need, device=f"cuda:{index}", dtype=torch.uint8) if need else None
+
+
+def _like(t, shape, dtype, given, name):
+    if given is None:
+        return t.new_empty(shape, dtype=dtype)
+    if given.shape != shape:
+        raise LotError(f"{name} must be {tuple(shape)}")
+    return given
 
 
 def lot_window_fwd(q, k, v, *, left, right=0, sinks=0, scale=None, key_len=None, q_start=None, out=None, lse=None, want_lse=False,
                    status=None, ws=None, stream=None):
     """Window attention with sinks.  scale None: d ** -0.5.  Returns (out, lse or None, ws or None)."""
     sizes = _band(q, k, v, key_len, q_start, left, right, sinks, scale)
-    _same_device(q, k=k, v=v, key_len=key_len, q_start=q_start, out=out, lse=lse, status=status, ws=ws)
-    with _guard(q):
-        if out is None:
-            out = torch.empty_like(q)
-        elif out.shape != q.shape:
-            raise LotError("out must have q's shape")
-        if lse is None and want_lse:
-            lse = torch.empty(q.shape[:3], device=q.device, dtype=torch.float32)
-        elif lse is not None and lse.shape != q.shape[:3]:
-            raise LotError("lse must be [B,H,nq]")
-        if ws is None:
-            need = lib().lot_window_fwd_workspace_bytes(*sizes[:10])
-            ws = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
-        i32, f32 = torch.int32, torch.float32
-        st = lib().lot_window_fwd(_dev(q, "q"), _dev(k, "k"), _dev(v, "v"), _dev(key_len, "key_len", i32), _dev(q_start, "q_start", i32), *sizes,
-                                  _dev(out, "out", q.dtype), _dev(lse, "lse", f32), _dev(status, "status", i32), _dev(ws, "ws"),
-                                  0 if ws is None else ws.numel(), _stream(stream))
+    L, dev, dt, i32 = lib(), q.get_device(), q.dtype, torch.int32
+    ptrs = (_ptr(q, "q", dt, dev), _ptr(k, "k", dt, dev), _ptr(v, "v", dt, dev), _ptr(key_len, "key_len", i32, dev), _ptr(q_start, "q_start", i32, dev))
+    out = _like(q, q.shape, dt, out, "out")
+    if want_lse or lse is not None:
+        lse = _like(q, q.shape[:3], torch.float32, lse, "lse")
+    ws = _work(ws, L.lot_window_fwd_workspace_bytes, sizes[:10], dev)
+    st = _call(L.lot_window_fwd, dev, (*ptrs, *sizes, _ptr(out, "out", dt, dev), _ptr(lse, "lse", torch.float32, dev), _ptr(status, "status", i32, dev),
+                                       _ptr(ws, "ws", torch.uint8, dev), 0 if ws is None else ws.numel(), _stream_of(stream, dev)))
     _check(st, "lot_window_fwd")
     return out, lse, ws
 
@@ -350,23 +370,16 @@ def lot_window_bwd(q, k, v, out, lse, dout, *, left, right=0, sinks=0, scale=Non
                    status=None, ws=None, stream=None):
     """Gradients of lot_window_fwd with respect to q, k, v.  Returns (dq, dk, dv, ws or None)."""
     sizes = _band(q, k, v, key_len, q_start, left, right, sinks, scale)
-    _same_device(q, k=k, v=v, out=out, lse=lse, dout=dout, key_len=key_len, q_start=q_start, dq=dq, dk=dk, dv=dv, status=status, ws=ws)
-    for name, t, like in (("out", out, q), ("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
-        if t is not None and t.shape != like.shape:
-            raise LotError(f"{name} must be {tuple(like.shape)}")
-    if lse.shape != q.shape[:3]:
-        raise LotError("lse must be [B,H,nq]")
-    with _guard(q):
-        dq = torch.empty_like(q) if dq is None else dq
-        dk = torch.empty_like(k) if dk is None else dk
-        dv = torch.empty_like(v) if dv is None else dv
-        if ws is None:
-            need = lib().lot_window_bwd_workspace_bytes(*sizes[:10])
-            ws = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
-        i32, dt = torch.int32, q.dtype
-        st = lib().lot_window_bwd(_dev(q, "q"), _dev(k, "k"), _dev(v, "v"), _dev(out, "out", dt), _dev(lse, "lse", torch.float32), _dev(dout, "dout", dt),
-                                  _dev(key_len, "key_len", i32), _dev(q_start, "q_start", i32), *sizes, _dev(dq, "dq", dt), _dev(dk, "dk", dt),
-                                  _dev(dv, "dv", dt), _dev(status, "status", i32), _dev(ws, "ws"), 0 if ws is None else ws.numel(), _stream(stream))
+    if out.shape != q.shape or dout.shape != q.shape or lse.shape != q.shape[:3]:
+        raise LotError("out and dout must have q's shape and lse be [B,H,nq]")
+    L, dev, dt, i32 = lib(), q.get_device(), q.dtype, torch.int32
+    ptrs = (_ptr(q, "q", dt, dev), _ptr(k, "k", dt, dev), _ptr(v, "v", dt, dev), _ptr(out, "out", dt, dev), _ptr(lse, "lse", torch.float32, dev),
+            _ptr(dout, "dout", dt, dev), _ptr(key_len, "key_len", i32, dev), _ptr(q_start, "q_start", i32, dev))
+    dq, dk, dv = _like(q, q.shape, dt, dq, "dq"), _like(k, k.shape, dt, dk, "dk"), _like(v, v.shape, dt, dv, "dv")
+    ws = _work(ws, L.lot_window_bwd_workspace_bytes, sizes[:10], dev)
+    st = _call(L.lot_window_bwd, dev, (*ptrs, *sizes, _ptr(dq, "dq", dt, dev), _ptr(dk, "dk", dt, dev), _ptr(dv, "dv", dt, dev),
+                                       _ptr(status, "status", i32, dev), _ptr(ws, "ws", torch.uint8, dev), 0 if ws is None else ws.numel(),
+                                       _stream_of(stream, dev)))
     _check(st, "lot_window_bwd")
     return dq, dk, dv, ws
 
@@ -382,32 +395,33 @@ def lot_cache4_empty(num_pages, Hkv, page_size, d, device) -> torch.Tensor:
     return torch.zeros(num_pages, Hkv, 2, page_size * (d // 2 + d // 8), device=device, dtype=torch.uint8)
 
 
-def _cache4(cache, pages, d, Hkv, **rows):
+def _cache4(cache, pages, B, d, Hkv, **rows):
     """(page_size, max_pages, num_pages) of a cache after its checks; rows: [B] tensors."""
-    if cache.dim() != 4 or cache.shape[2] != 2 or cache.shape[1] != Hkv or pages.dim() != 2:
+    if cache.dim() != 4 or pages.dim() != 2:
+        raise LotError("cache must be [num_pages,Hkv,2,page_size*(d/2+d/8)] and pages [B,max_pages]")
+    (num_pages, heads, sides, size), (batch, max_pages) = cache.shape, pages.shape
+    if sides != 2 or heads != Hkv or batch != B:
         raise LotError("cache must be [num_pages,Hkv,2,page_size*(d/2+d/8)] and pages [B,max_pages]")
     per = d // 2 + d // 8
-    if per == 0 or cache.shape[3] % per:
+    if per == 0 or size % per:
         raise LotError(f"cache rows do not fit d = {d}")
     for name, t in rows.items():
-        if t is not None and t.shape != (pages.shape[0],):
+        if t is not None and t.shape != (B,):
             raise LotError(f"{name} must be [B]")
-    return cache.shape[3] // per, pages.shape[1], cache.shape[0]
+    return size // per, max_pages, num_pages
 
 
 def lot_cache4_write(cache, pages, k, v, start, *, count=None, status=None, stream=None):
     """Tokens k, v [B,Hkv,m,d] into the cache at positions start[b] and on.  Returns cache."""
-    if k.dim() != 4 or v.shape != k.shape or v.dtype is not k.dtype:
-        raise LotError("k, v must be [B,Hkv,m,d] of one dtype")
+    if k.dim() != 4 or v.shape != k.shape:
+        raise LotError("k, v must be [B,Hkv,m,d]")
     B, Hkv, m, d = k.shape
-    sizes = _cache4(cache, pages, d, Hkv, start=start, count=count)
-    if pages.shape[0] != B:
-        raise LotError("pages must be [B,max_pages]")
-    _same_device(k, v=v, cache=cache, pages=pages, start=start, count=count, status=status)
-    i32 = torch.int32
-    with _guard(k):
-        st = lib().lot_cache4_write(_dev(k, "k"), _dev(v, "v"), _dev(pages, "pages", i32), _dev(start, "start", i32), _dev(count, "count", i32),
-                                    _dtype_code(k), B, Hkv, m, d, *sizes, _dev(cache, "cache", torch.uint8), _dev(status, "status", i32), _stream(stream))
+    page_size, max_pages, num_pages = _cache4(cache, pages, B, d, Hkv, start=start, count=count)
+    dev, dt, i32 = k.get_device(), k.dtype, torch.int32
+    st = _call(lib().lot_cache4_write, dev, (
+        _ptr(k, "k", dt, dev), _ptr(v, "v", dt, dev), _ptr(pages, "pages", i32, dev), _ptr(start, "start", i32, dev), _ptr(count, "count", i32, dev),
+        _dtype_code(k), B, Hkv, m, d, page_size, max_pages, num_pages, _ptr(cache, "cache", torch.uint8, dev), _ptr(status, "status", i32, dev),
+        _stream_of(stream, dev)))
     _check(st, "lot_cache4_write")
     return cache
 
@@ -415,16 +429,14 @@ def lot_cache4_write(cache, pages, k, v, start, *, count=None, status=None, stre
 def lot_cache4_read(cache, pages, start, m, *, d, dtype=torch.bfloat16, count=None, k=None, v=None, status=None, stream=None):
     """Tokens start[b] .. start[b] + m - 1 of every sequence as k, v [B,Hkv,m,d].  Returns (k, v)."""
     B, Hkv = pages.shape[0], cache.shape[1]
-    sizes = _cache4(cache, pages, d, Hkv, start=start, count=count)
-    _same_device(cache, pages=pages, start=start, count=count, k=k, v=v, status=status)
-    i32 = torch.int32
-    with _guard(cache):
-        k = torch.empty(B, Hkv, m, d, device=cache.device, dtype=dtype) if k is None else k
-        v = torch.empty(B, Hkv, m, d, device=cache.device, dtype=dtype) if v is None else v
-        if k.shape != (B, Hkv, m, d) or v.shape != k.shape:
-            raise LotError("k, v must be [B,Hkv,m,d]")
-        st = lib().lot_cache4_read(_dev(cache, "cache", torch.uint8), _dev(pages, "pages", i32), _dev(start, "start", i32), _dev(count, "count", i32),
-                                   _dtype_code(k), B, Hkv, m, d, *sizes, _dev(k, "k"), _dev(v, "v", k.dtype), _dev(status, "status", i32), _stream(stream))
+    page_size, max_pages, num_pages = _cache4(cache, pages, B, d, Hkv, start=start, count=count)
+    dev, i32, shape = cache.get_device(), torch.int32, (B, Hkv, m, d)
+    k = _like(cache, shape, dtype, k, "k")
+    v = _like(cache, shape, k.dtype, v, "v")
+    st = _call(lib().lot_cache4_read, dev, (
+        _ptr(cache, "cache", torch.uint8, dev), _ptr(pages, "pages", i32, dev), _ptr(start, "start", i32, dev), _ptr(count, "count", i32, dev),
+        _dtype_code(k), B, Hkv, m, d, page_size, max_pages, num_pages, _ptr(k, "k", k.dtype, dev), _ptr(v, "v", k.dtype, dev),
+        _ptr(status, "status", i32, dev), _stream_of(stream, dev)))
     _check(st, "lot_cache4_read")
     return k, v
 
@@ -436,26 +448,16 @@ def lot_cache4_attention(q, cache, pages, length, *, left=-1, sinks=0, scale=Non
         raise LotError("q must be [B,H,nq,d]")
     B, H, nq, d = q.shape
     Hkv = cache.shape[1]
-    page_size, max_pages, num_pages = _cache4(cache, pages, d, Hkv, length=length)
-    if pages.shape[0] != B:
-        raise LotError("pages must be [B,max_pages]")
-    _same_device(q, cache=cache, pages=pages, length=length, out=out, lse=lse, status=status, ws=ws)
-    code, i32 = _dtype_code(q), torch.int32
-    with _guard(q):
-        if out is None:
-            out = torch.empty_like(q)
-        elif out.shape != q.shape:
-            raise LotError("out must have q's shape")
-        if lse is None and want_lse:
-            lse = torch.empty(q.shape[:3], device=q.device, dtype=torch.float32)
-        elif lse is not None and lse.shape != q.shape[:3]:
-            raise LotError("lse must be [B,H,nq]")
-        if ws is None:
-            need = lib().lot_cache4_attention_workspace_bytes(code, B, H, Hkv, nq, d, page_size, max_pages, int(left), int(sinks))
-            ws = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
-        st = lib().lot_cache4_attention(_dev(q, "q"), _dev(cache, "cache", torch.uint8), _dev(pages, "pages", i32), _dev(length, "length", i32),
-                                        code, B, H, Hkv, nq, d, page_size, max_pages, num_pages, int(left), int(sinks),
-                                        float(d ** -0.5 if scale is None else scale), _dev(out, "out", q.dtype), _dev(lse, "lse", torch.float32),
-                                        _dev(status, "status", i32), _dev(ws, "ws"), 0 if ws is None else ws.numel(), _stream(stream))
+    page_size, max_pages, num_pages = _cache4(cache, pages, B, d, Hkv, length=length)
+    L, dev, dt, i32, code, left, sinks = lib(), q.get_device(), q.dtype, torch.int32, _dtype_code(q), int(left), int(sinks)
+    ptrs = (_ptr(q, "q", dt, dev), _ptr(cache, "cache", torch.uint8, dev), _ptr(pages, "pages", i32, dev), _ptr(length, "length", i32, dev))
+    out = _like(q, q.shape, dt, out, "out")
+    if want_lse or lse is not None:
+        lse = _like(q, q.shape[:3], torch.float32, lse, "lse")
+    ws = _work(ws, L.lot_cache4_attention_workspace_bytes, (code, B, H, Hkv, nq, d, page_size, max_pages, left, sinks), dev)
+    st = _call(L.lot_cache4_attention, dev, (
+        *ptrs, code, B, H, Hkv, nq, d, page_size, max_pages, num_pages, left, sinks, float(d ** -0.5 if scale is None else scale),
+        _ptr(out, "out", dt, dev), _ptr(lse, "lse", torch.float32, dev), _ptr(status, "status", i32, dev), _ptr(ws, "ws", torch.uint8, dev),
+        0 if ws is None else ws.numel(), _stream_of(stream, dev)))
     _check(st, "lot_cache4_attention")
     return out, lse, ws

@@ -1,10 +1,11 @@
 // The 4-bit cache: tokens quantised as they are written, and read back.
 //
 // A group of 32 channels of a token and head is held as s = bf16((hi - lo) / 15), z = bf16(lo) and codes round((x - z) / s), half to even.
-// Four lanes share a group, eight channels each.  The quotients are taken in float32; where one comes so near to the border between two
-// results that its rounding could fall on the other side, it is taken in float64, so that what is stored depends on the definition alone.
-// Both kernels are bound by what they read and write; a warp takes neighbouring tokens (by their place in the cache, so that the two
-// tokens whose value codes share words are neighbours in it) and stores whole words.
+// The quotients are taken in float32; where one comes so near to the border between two results that its rounding could fall on the
+// other side, it is taken in float64, so that what is stored depends on the definition alone.
+// A warp takes a block of 16 places of one head and side, which lies in one page: a lane eight channels of every group of two tokens, so that
+// rows are read and written in 64-byte pieces and codes in whole words; the values' codes change from the tokens' order to the operands'
+// by three exchanges between lanes.
 #include "lot_window.cuh"
 
 #include <type_traits>
@@ -15,22 +16,54 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// What float32 cannot decide, out of line: only groups next to a border of the scale, or of magnitudes near the type's ends, come here.
+__device__ __noinline__ float exact_scale(float lo, float hi) { return (float)(((double)hi - (double)lo) / 15.0); }
+__device__ __noinline__ uint32_t exact_code(float x, float z, float s) { return (uint32_t)fmin(fmax(rint(((double)x - (double)z) / (double)s), 0.0), 15.0); }
+
 // scale of a group: ((hi - lo) / 15) rounded to float32 and then to bf16, as the bits of the bf16
 __device__ __forceinline__ uint32_t scale_bits(float lo, float hi)
 {
-    const float q = __fdiv_rn(hi - lo, 15.f);
+    const float q = (hi - lo) * (1.f / 15.f);
     uint32_t u = __float_as_uint(q);
     const uint32_t low = u & 0xffffu;
-    // q is within 2 ulp of the exact quotient: only next to the middle between two bf16 numbers can that matter
-    if ((low >= 0x7ffcu && low <= 0x8004u) || !(q < 1e30f) || q < 1e-30f) u = __float_as_uint((float)(((double)hi - (double)lo) / 15.0));
+    // q is within 3 ulp of the exact quotient: only next to the middle between two bf16 numbers can that matter
+    if ((low >= 0x7ff8u && low <= 0x8008u) || !(q < 1e30f) || (q < 1e-30f && hi != lo)) u = __float_as_uint(exact_scale(lo, hi));
     return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
 }
-__device__ __forceinline__ uint32_t code_of(float x, float z, float s, float inv)
+// The code of x when (x - z) / s is next to h = code + 1/2: the sign of x - z - h s.  d + e is x - z exactly, h s (13 bits) is exact and so is
+// its difference with d, which it nearly equals.  bf16 tensors, whose differences and scales have few bits, come exactly between two
+// codes in one of 500 channels.
+__device__ __forceinline__ uint32_t border_code(float x, float z, float s, float r)
 {
-    const float r = (x - z) * inv;                             // within 1e-5 of the exact quotient where s is in the ordinary range
-    float n = rintf(r);
-    if (fabsf(fabsf(r - n) - 0.5f) < 1e-4f || s < 1e-30f || s > 1e30f) n = (float)rint(((double)x - (double)z) / (double)s);
-    return (uint32_t)fminf(fmaxf(n, 0.f), 15.f);
+    const float below = floorf(r), hs = (below + 0.5f) * s, d = x - z, b = d - x, e = (x - (d - b)) - (z + b), t = (d - hs) + e;
+    const uint32_t n = (uint32_t)below;
+    return t > 0.f ? n + 1u : t < 0.f ? n : n + (n & 1u);
+}
+// codes of eight channels; s > 0
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], float z, float s)
+{
+    constexpr float kWhole = 12582912.f;                       // 1.5 x 2^23: adding it rounds to a whole number, half to even, in the low bits
+    const float inv = __frcp_rn(s);
+    float r[8], near = 1.f;
+    uint32_t codes = 0;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        // three roundings: within 15.1 x 3 x 2^-24 = 2.7e-6 of the exact quotient where that is between the codes
+        r[c] = fminf(fmaxf((x[c] - z) * inv, 0.f), 15.f);
+        const float w = r[c] + kWhole;
+        near = fminf(near, fabsf(fabsf(r[c] - (w - kWhole)) - 0.5f));
+        codes |= (__float_as_uint(w) & 15u) << (4 * c);
+    }
+    if (s < 1e-30f || s > 1e30f) {
+        codes = 0;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) codes |= exact_code(x[c], z, s) << (4 * c);
+    } else if (near < 4e-6f) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+            if (fabsf(r[c] - floorf(r[c]) - 0.5f) < 4e-6f) codes = (codes & ~(15u << (4 * c))) | border_code(x[c], z, s, r[c]) << (4 * c);
+    }
+    return codes;
 }
 
 __device__ __forceinline__ void load8(const float *p, float (&v)[8])
@@ -64,146 +97,163 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&v)[8])
 struct Rows {
     Cache4 c;
     const int32_t *start, *count;
-    int m;
+    int m, blocks;                         // blocks of 16 places that m tokens may touch
     int *status;
 };
 
-// The token of this thread: its index in the call (or -1: none here), page and place.  Threads of a token and of its pair agree.
-struct Token {
-    int i, page, at;
+// A warp's block of 16 places: (side, head, block) by its number within the batch row.
+struct Block {
+    int side, head, first, m, at, page;    // first: the call's token at the block's first place (may be negative); m tokens in all; page < 0: none
+    __device__ __forceinline__ bool has(int j) const { return first + j >= 0 && first + j < m; }
+    __device__ __forceinline__ bool any() const { return first < m && first > -kBlockTokens; }
 };
-__device__ __forceinline__ Token token_of(const Rows &r, int b, int slot)
+__device__ __forceinline__ Block block_of(const Rows &r, int b, int n, int lane)
 {
-    const int start = r.start[b], m = r.count != nullptr ? min(max(r.count[b], 0), r.m) : r.m;
-    const long long pos = (long long)start - (start & 1) + slot;      // pairs of places begin at even ones
-    Token t{(int)(pos - start), 0, 0};
-    if (pos < start || t.i >= m) { t.i = -1; return t; }
-    if (pos < 0 || pos >= (long long)r.c.max_pages * r.c.page_size) {
-        if (r.status != nullptr) atomicOr(r.status, 32 /* LOT_DEV_PAGE */);
-        t.i = -1;
-        return t;
+    Block k;
+    const int rows = r.blocks * r.c.Hkv, x = n % rows, start = r.start[b];
+    k.side = n / rows;
+    k.head = x / r.blocks;
+    k.m = r.count != nullptr ? min(max(r.count[b], 0), r.m) : r.m;
+    const long long pos = ((long long)start >> 4) * kBlockTokens + (long long)(x % r.blocks) * kBlockTokens;
+    k.first = (int)(pos - start);
+    k.at = 0;
+    k.page = -1;
+    if (k.side > 1 || !k.any()) { k.m = 0; return k; }
+    if (pos >= 0 && pos < (long long)r.c.max_pages * r.c.page_size) {
+        k.at = (int)pos % r.c.page_size;
+        k.page = r.c.pages[(size_t)b * r.c.max_pages + (int)pos / r.c.page_size];
+        if (k.page >= r.c.num_pages) k.page = -1;
     }
-    t.page = r.c.pages[(size_t)b * r.c.max_pages + (int)pos / r.c.page_size];
-    t.at = (int)pos % r.c.page_size;
-    if (t.page < 0 || t.page >= r.c.num_pages) {
-        if (r.status != nullptr) atomicOr(r.status, 32);
-        t.page = -1;
-    }
-    return t;
+    if (k.page < 0 && lane == 0 && r.status != nullptr) atomicOr(r.status, 32 /* LOT_DEV_PAGE */);
+    return k;
 }
 
-// The four lanes of a group hold 32-bit words of eight nibbles, nibble x of lane t for channel 8 t + x; back come the halves of g = 2 t
-// (low) and 2 t + 1 (high), whose nibble i is the one of lane i.  Its own inverse up to the roles of the words.
-__device__ __forceinline__ uint32_t across(uint32_t w, int t)
+// Lane 4 x + t, x = 4 e + i, holds words of eight nibbles: token 2 t + e, channels 8 i .. 8 i + 7 of a group.  Afterwards it holds the same
+// group's stored word of lane (g, t), g = x: nibble 4 e + i is token 2 t + e's channel 8 i + g.  Three exchanges, each of one bit of x with
+// one bit of the nibble's number; its own inverse.
+__device__ __forceinline__ uint32_t exchange(uint32_t w, int lane)
 {
-    uint32_t lo = 0, hi = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t y = __shfl_sync(0xffffffffu, w, i, 4) >> (8 * t);
-        lo |= (y & 15u) << (4 * i);
-        hi |= ((y >> 4) & 15u) << (4 * i);
-    }
-    return lo | (hi << 16);
+    const uint32_t a = __shfl_xor_sync(0xffffffffu, w, 4);
+    w = lane & 4 ? (w & 0xf0f0f0f0u) | ((a >> 4) & 0x0f0f0f0fu) : (w & 0x0f0f0f0fu) | ((a << 4) & 0xf0f0f0f0u);
+    const uint32_t b = __shfl_xor_sync(0xffffffffu, w, 8);
+    w = lane & 8 ? (w & 0xff00ff00u) | ((b >> 8) & 0x00ff00ffu) : (w & 0x00ff00ffu) | ((b << 8) & 0xff00ff00u);
+    const uint32_t c = __shfl_xor_sync(0xffffffffu, w, 16);
+    return lane & 16 ? (w & 0xffff0000u) | (c >> 16) : (w & 0x0000ffffu) | (c << 16);
 }
-// nibble x of lane t from the halves of across(): half g stands in lane g / 2
-__device__ __forceinline__ uint32_t back(uint32_t h, int t)
+
+template <int W> struct Words;
+template <> struct Words<1> { typedef uint32_t T; };
+template <> struct Words<2> { typedef uint2 T; };
+template <> struct Words<4> { typedef uint4 T; };
+template <int W> __device__ __forceinline__ void store_words(void *p, const uint32_t (&w)[W])
 {
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t y = __shfl_sync(0xffffffffu, h, i, 4) >> (4 * t);
-        w |= ((y & 15u) | ((y >> 16) & 15u) << 4) << (8 * i);
-    }
-    return w;
+    typename Words<W>::T v;
+    memcpy(&v, w, sizeof v);
+    *static_cast<typename Words<W>::T *>(p) = v;
+}
+template <int W> __device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[W])
+{
+    const typename Words<W>::T v = __ldg(static_cast<const typename Words<W>::T *>(p));
+    memcpy(w, &v, sizeof v);
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__ Rows r, const T *k, const T *v)
 {
-    constexpr int W = D / kGroup, LANES = D / 8;               // lanes of a token
-    const int head = blockIdx.y, b = blockIdx.z >> 1, side = blockIdx.z & 1;
-    const int slot = (int)((blockIdx.x * kThreads + threadIdx.x) / LANES), lane = threadIdx.x % LANES, w = lane >> 2, t = lane & 3;
-    const Token tok = token_of(r, b, slot);
-    const bool here = tok.i >= 0 && tok.page >= 0;
-    float x[8];
+    constexpr int W = D / kGroup;
+    const int lane = threadIdx.x & 31, b = blockIdx.y, t = lane & 3, i = (lane >> 2) & 3, e = lane >> 4;
+    const int warp = (int)(blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)), u = warp & 1, j = 8 * u + 2 * t + e;      // half a block
+    const Block blk = block_of(r, b, warp >> 1, lane);
+    if (blk.m == 0 || blk.page < 0) return;
+    const T *x0 = (blk.side ? v : k) + ((size_t)b * r.c.Hkv + blk.head) * r.m * D;
+    float x[W][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    if (here) load8((side ? v : k) + (((size_t)b * r.c.Hkv + head) * r.m + tok.i) * D + lane * 8, x);
-    float lo = x[0], hi = x[0];
-    uint32_t big = __float_as_uint(x[0]) & 0x7fffffffu;
+    for (int w = 0; w < W; ++w) {
+        if (blk.has(j)) {
+            load8(x0 + (size_t)(blk.first + j) * D + w * kGroup + i * 8, x[w]);
+        } else {
 #pragma unroll
-    for (int e = 1; e < 8; ++e) {
-        lo = fminf(lo, x[e]);
-        hi = fmaxf(hi, x[e]);
-        big = max(big, __float_as_uint(x[e]) & 0x7fffffffu);
-    }
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
-    }
-    uint32_t param = 0x7fc07fc0u, codes = 0;                   // a value that is not finite: NaN for the group
-    if (big < 0x7f800000u) {
-        const uint32_t sb = scale_bits(lo, hi);
-        const float s = __uint_as_float(sb << 16);
-        const uint32_t zb = __float_as_uint(lo), zr = (zb + 0x7fffu + ((zb >> 16) & 1u)) & 0xffff0000u;
-        const float z = __uint_as_float(zr);
-        param = sb | zr;
-        if (s > 0.f) {
-            const float inv = __frcp_rn(s);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) codes |= code_of(x[e], z, s, inv) << (4 * e);
+            for (int c = 0; c < 8; ++c) x[w][c] = 0.f;
         }
     }
-    uint8_t *base = side_base(r.c, here ? tok.page : 0, head, side);
-    if (here && t == 0) reinterpret_cast<uint32_t *>(base + (size_t)r.c.page_size * (D / 2))[(size_t)tok.at * W + w] = param;
-    if (side == 0) {
-        if (here) *reinterpret_cast<uint32_t *>(base + (size_t)tok.at * (D / 2) + (t * W + w) * 4) = codes;
+    uint8_t *base = side_base(r.c, blk.page, blk.head, blk.side);
+    uint32_t *params = reinterpret_cast<uint32_t *>(base + (size_t)r.c.page_size * (D / 2));
+    uint32_t codes[W], param[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        float lo = x[w][0], hi = lo;
+        uint32_t big = __float_as_uint(lo) & 0x7fffffffu;
+#pragma unroll
+        for (int c = 1; c < 8; ++c) {
+            lo = fminf(lo, x[w][c]);
+            hi = fmaxf(hi, x[w][c]);
+            big = max(big, __float_as_uint(x[w][c]) & 0x7fffffffu);
+        }
+#pragma unroll
+        for (int o = 4; o < 16; o <<= 1) {                 // the group's four lanes
+            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+        }
+        codes[w] = 0;
+        param[w] = 0x7fc07fc0u;                            // a value that is not finite: NaN for the group
+        if (big < 0x7f800000u) {
+            const uint32_t sb = scale_bits(lo, hi), zb = __float_as_uint(lo), zr = (zb + 0x7fffu + ((zb >> 16) & 1u)) & 0xffff0000u;
+            const float s = __uint_as_float(sb << 16), z = __uint_as_float(zr);
+            param[w] = sb | zr;
+            if (s > 0.f) codes[w] = codes_of(x[w], z, s);
+        }
+    }
+    if (blk.has(j) && i == 0) store_words(params + (size_t)(blk.at + j) * W, param);
+    if (blk.side == 0) {
+        if (blk.has(j)) store_words(base + (size_t)(blk.at + j) * (D / 2) + i * 4 * W, codes);
         return;
     }
-    const uint32_t halves = across(codes, t), other = __shfl_xor_sync(0xffffffffu, halves, LANES);       // the pair's token
-    const int pair = __shfl_xor_sync(0xffffffffu, here ? 1 : 0, LANES);
-    if (!here) return;
-    const int odd = slot & 1;
-    if (pair) {                                                // the even token's lanes store g = 2 t of both, the odd one's 2 t + 1
-        const uint32_t word = odd ? (other >> 16) | (halves & 0xffff0000u) : (halves & 0xffffu) | (other << 16);
-        *reinterpret_cast<uint32_t *>(base + value_half(tok.at & ~1, 2 * t + odd, w, W)) = word;
-    } else {
-        *reinterpret_cast<uint16_t *>(base + value_half(tok.at, 2 * t, w, W)) = (uint16_t)halves;
-        *reinterpret_cast<uint16_t *>(base + value_half(tok.at, 2 * t + 1, w, W)) = (uint16_t)(halves >> 16);
+#pragma unroll
+    for (int w = 0; w < W; ++w) codes[w] = exchange(codes[w], lane);
+    uint8_t *o = base + value_half(blk.at + 8 * u + 2 * t, lane >> 2, 0, W);
+    const bool even = blk.has(8 * u + 2 * t), odd = blk.has(8 * u + 2 * t + 1);
+    if (even && odd) {
+        store_words(o, codes);
+    } else if (even || odd) {
+#pragma unroll
+        for (int w = 0; w < W; ++w) *reinterpret_cast<uint16_t *>(o + 4 * w + (odd ? 2 : 0)) = (uint16_t)(odd ? codes[w] >> 16 : codes[w]);
     }
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ Rows r, T *k, T *v)
 {
-    constexpr int W = D / kGroup, LANES = D / 8;
-    const int head = blockIdx.y, b = blockIdx.z >> 1, side = blockIdx.z & 1;
-    const int slot = (int)((blockIdx.x * kThreads + threadIdx.x) / LANES), lane = threadIdx.x % LANES, w = lane >> 2, t = lane & 3;
-    const int start = r.start[b], m = r.count != nullptr ? min(max(r.count[b], 0), r.m) : r.m;
-    const int i = slot - (start & 1);
-    const Token tok = token_of(r, b, slot);
-    const bool here = tok.i >= 0 && tok.page >= 0;
-    const uint8_t *base = side_base(r.c, here ? tok.page : 0, head, side);
-    uint32_t param = 0, codes = 0;
-    if (here) {
-        param = __ldg(reinterpret_cast<const uint32_t *>(base + (size_t)r.c.page_size * (D / 2)) + (size_t)tok.at * W + w);
-        if (side == 0) {
-            codes = __ldg(reinterpret_cast<const uint32_t *>(base + (size_t)tok.at * (D / 2) + (t * W + w) * 4));
-        } else {                                               // words of g = 2 t, 2 t + 1 hold both tokens of the pair
-            const uint32_t p = __ldg(reinterpret_cast<const uint32_t *>(base + value_half(tok.at & ~1, 2 * t, w, W)));
-            const uint32_t q = __ldg(reinterpret_cast<const uint32_t *>(base + value_half(tok.at & ~1, 2 * t + 1, w, W)));
-            codes = (tok.at & 1) ? (p >> 16) | (q & 0xffff0000u) : (p & 0xffffu) | (q << 16);
+    constexpr int W = D / kGroup;
+    const int lane = threadIdx.x & 31, b = blockIdx.y, t = lane & 3, i = (lane >> 2) & 3, e = lane >> 4;
+    const Block blk = block_of(r, b, (int)(blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)), lane);
+    if (blk.m == 0) return;
+    uint32_t codes[2][W], param[2][W];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int j = 8 * u + 2 * t + e;
+#pragma unroll
+        for (int w = 0; w < W; ++w) codes[u][w] = param[u][w] = 0;
+        if (blk.page < 0) continue;                            // a token whose page is missing reads as zeros
+        const uint8_t *base = side_base(r.c, blk.page, blk.head, blk.side);
+        load_words(reinterpret_cast<const uint32_t *>(base + (size_t)r.c.page_size * (D / 2)) + (size_t)(blk.at + j) * W, param[u]);
+        load_words(blk.side ? base + value_half(blk.at + 8 * u + 2 * t, lane >> 2, 0, W) : base + (size_t)(blk.at + j) * (D / 2) + i * 4 * W, codes[u]);
+    }
+    T *x0 = (blk.side ? v : k) + ((size_t)b * r.c.Hkv + blk.head) * r.m * D;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int j = 8 * u + 2 * t + e;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (blk.side) codes[u][w] = exchange(codes[u][w], lane);
+            if (!blk.has(j)) continue;
+            const float s = param_scale(param[u][w]), z = param_least(param[u][w]);
+            float x[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) x[c] = fmaf(s, (float)((codes[u][w] >> (4 * c)) & 15u), z);
+            store8(x0 + (size_t)(blk.first + j) * D + w * kGroup + i * 8, x);
         }
     }
-    if (side == 1) codes = back(codes, t);
-    if (i < 0 || i >= m) return;                               // a token whose page is missing reads as zeros
-    const float s = param_scale(param), z = param_least(param);
-    float x[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = fmaf(s, (float)((codes >> (4 * e)) & 15u), z);
-    store8((side ? v : k) + (((size_t)b * r.c.Hkv + head) * r.m + i) * D + lane * 8, x);
 }
 
 template <typename F> cudaError_t by_width(int dtype, int d, F f)
@@ -211,7 +261,9 @@ template <typename F> cudaError_t by_width(int dtype, int d, F f)
     if (dtype == 0) return d == 32 ? f(float{}, std::integral_constant<int, 32>{}) : d == 64 ? f(float{}, std::integral_constant<int, 64>{}) : f(float{}, std::integral_constant<int, 128>{});
     return d == 32 ? f(__nv_bfloat16{}, std::integral_constant<int, 32>{}) : d == 64 ? f(__nv_bfloat16{}, std::integral_constant<int, 64>{}) : f(__nv_bfloat16{}, std::integral_constant<int, 128>{});
 }
-dim3 grid_of(const Cache4 &c, int B, int m) { return dim3((unsigned)(((long long)m + 1) * (c.d / 8) + kThreads - 1) / kThreads, c.Hkv, 2 * B); }
+int blocks_of(int m) { return (int)(((long long)m + 2 * (kBlockTokens - 1)) / kBlockTokens); }
+// per: warps a block of places
+dim3 grid_of(const Cache4 &c, int B, int m, int per) { return dim3((unsigned)((2ll * c.Hkv * blocks_of(m) * per + kThreads / 32 - 1) / (kThreads / 32)), B); }
 
 } // namespace
 
@@ -220,7 +272,7 @@ cudaError_t launch_write4(const Cache4 &c, const void *k, const void *v, const i
 {
     return by_width(dtype, c.d, [&](auto t, auto width) {
         using T = decltype(t);
-        write_kernel<T, decltype(width)::value><<<grid_of(c, B, m), kThreads, 0, st>>>(Rows{c, start, count, m, status}, static_cast<const T *>(k), static_cast<const T *>(v));
+        write_kernel<T, decltype(width)::value><<<grid_of(c, B, m, 2), kThreads, 0, st>>>(Rows{c, start, count, m, blocks_of(m), status}, static_cast<const T *>(k), static_cast<const T *>(v));
         return cudaGetLastError();
     });
 }
@@ -229,7 +281,7 @@ cudaError_t launch_read4(const Cache4 &c, void *k, void *v, const int32_t *start
 {
     return by_width(dtype, c.d, [&](auto t, auto width) {
         using T = decltype(t);
-        read_kernel<T, decltype(width)::value><<<grid_of(c, B, m), kThreads, 0, st>>>(Rows{c, start, count, m, status}, static_cast<T *>(k), static_cast<T *>(v));
+        read_kernel<T, decltype(width)::value><<<grid_of(c, B, m, 1), kThreads, 0, st>>>(Rows{c, start, count, m, blocks_of(m), status}, static_cast<T *>(k), static_cast<T *>(v));
         return cudaGetLastError();
     });
 }
