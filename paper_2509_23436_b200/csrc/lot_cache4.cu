@@ -30,54 +30,144 @@ __device__ __forceinline__ uint32_t scale_bits(float lo, float hi)
     if ((low >= 0x7ff8u && low <= 0x8008u) || !(q < 1e30f) || (q < 1e-30f && hi != lo)) u = __float_as_uint(exact_scale(lo, hi));
     return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
 }
-// The code of x when (x - z) / s is next to h = code + 1/2: the sign of x - z - h s.  d + e is x - z exactly, h s (13 bits) is exact and so is
+// The code of x when (x - z) / s is next to h = below + 1/2: the sign of x - z - h s.  d + e is x - z exactly, h s (13 bits) is exact and so is
 // its difference with d, which it nearly equals.  bf16 tensors, whose differences and scales have few bits, come exactly between two
 // codes in one of 500 channels.
-__device__ __forceinline__ uint32_t border_code(float x, float z, float s, float r)
+__device__ __forceinline__ uint32_t border_code(float x, float z, float s, float below)
 {
-    const float below = floorf(r), hs = (below + 0.5f) * s, d = x - z, b = d - x, e = (x - (d - b)) - (z + b), t = (d - hs) + e;
+    const float hs = (below + 0.5f) * s, d = x - z, b = d - x, e = (x - (d - b)) - (z + b), t = (d - hs) + e;
     const uint32_t n = (uint32_t)below;
     return t > 0.f ? n + 1u : t < 0.f ? n : n + (n & 1u);
 }
-// codes of eight channels; s > 0
-__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], float z, float s)
+// Codes of eight channels; s > 0.  clamp: quotients may lie outside 0 .. 15.5 (a least value that was rounded to bf16).
+template <bool CLAMP> __device__ __forceinline__ uint32_t codes_of(const float (&x)[8], float z, float s)
 {
-    constexpr float kWhole = 12582912.f;                       // 1.5 x 2^23: adding it rounds to a whole number, half to even, in the low bits
-    const float inv = __frcp_rn(s);
-    float r[8], near = 1.f;
-    uint32_t codes = 0;
+    constexpr float kWhole = 12582912.f;                       // 1.5 x 2^23: adding it rounds to a whole number, half to even
+    constexpr float kNear = 0.5f - 6e-6f;                      // three roundings and an approximate reciprocal: within 15.1 x 4 x 2^-24 = 3.6e-6
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    const f2 inv2 = pack2(inv, inv), z2 = pack2(-z, -z), whole = pack2(kWhole, kWhole), back = pack2(-kWhole, -kWhole), minus = pack2(-1.f, -1.f);
+    f2 n[4], off[4];                                           // channels c and c + 4
+    float near = 0.f;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        // three roundings: within 15.1 x 3 x 2^-24 = 2.7e-6 of the exact quotient where that is between the codes
-        r[c] = fminf(fmaxf((x[c] - z) * inv, 0.f), 15.f);
-        const float w = r[c] + kWhole;
-        near = fminf(near, fabsf(fabsf(r[c] - (w - kWhole)) - 0.5f));
-        codes |= (__float_as_uint(w) & 15u) << (4 * c);
+    for (int c = 0; c < 4; ++c) {
+        f2 r = mul2(add2(pack2(x[c], x[c + 4]), z2), inv2);
+        if (CLAMP) {
+            float u, v;
+            unpack2(r, u, v);
+            r = pack2(fminf(fmaxf(u, 0.f), 15.f), fminf(fmaxf(v, 0.f), 15.f));
+        }
+        n[c] = add2(add2(r, whole), back);
+        off[c] = fma2(n[c], minus, r);
+        float u, v;
+        unpack2(off[c], u, v);
+        near = fmaxf(near, fmaxf(fabsf(u), fabsf(v)));
     }
+    // four codes in one number below 2^16, exactly
+    const f2 by16 = pack2(16.f, 16.f), word = add2(fma2(fma2(n[3], by16, n[2]), pack2(256.f, 256.f), fma2(n[1], by16, n[0])), pack2(8388608.f, 8388608.f));
+    float lo, hi;
+    unpack2(word, lo, hi);
+    uint32_t codes = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410);
     if (s < 1e-30f || s > 1e30f) {
         codes = 0;
 #pragma unroll
         for (int c = 0; c < 8; ++c) codes |= exact_code(x[c], z, s) << (4 * c);
-    } else if (near < 4e-6f) {
+    } else if (near > kNear) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-            if (fabsf(r[c] - floorf(r[c]) - 0.5f) < 4e-6f) codes = (codes & ~(15u << (4 * c))) | border_code(x[c], z, s, r[c]) << (4 * c);
+        for (int c = 0; c < 4; ++c) {
+            float u, v, m, w;
+            unpack2(off[c], u, v);
+            unpack2(n[c], m, w);
+            if (fabsf(u) > kNear) codes = (codes & ~(15u << (4 * c))) | border_code(x[c], z, s, u > 0.f ? m : m - 1.f) << (4 * c);
+            if (fabsf(v) > kNear) codes = (codes & ~(15u << (4 * c + 16))) | border_code(x[c + 4], z, s, v > 0.f ? w : w - 1.f) << (4 * c + 16);
+        }
     }
     return codes;
 }
 
-__device__ __forceinline__ void load8(const float *p, float (&v)[8])
+// least and largest of eight channels; NaN if one is
+__device__ __forceinline__ float min_nan(float a, float b)
 {
-    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&v)[8])
+__device__ __forceinline__ float max_nan(float a, float b)
 {
-    const uint4 a = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t min_nan2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_nan2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// Eight channels of a lane as they were loaded, and the least and largest of its group (lanes 4 and 8 apart).
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+    float x[8];
+    __device__ __forceinline__ void load(const float *p)
+    {
+        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
+        for (int c = 0; c < 8; ++c) x[c] = 0.f;
+    }
+    __device__ __forceinline__ void range(float &lo, float &hi) const
+    {
+        lo = min_nan(min_nan(min_nan(x[0], x[1]), min_nan(x[2], x[3])), min_nan(min_nan(x[4], x[5]), min_nan(x[6], x[7])));
+        hi = max_nan(max_nan(max_nan(x[0], x[1]), max_nan(x[2], x[3])), max_nan(max_nan(x[4], x[5]), max_nan(x[6], x[7])));
+#pragma unroll
+        for (int o = 4; o < 16; o <<= 1) {
+            lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+            hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = x[c];
+    }
+};
+template <> struct Eight<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p)
+    {
+        const uint4 a = *reinterpret_cast<const uint4 *>(p);
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+    }
+    __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0u; }
+    __device__ __forceinline__ void range(float &lo, float &hi) const
+    {
+        uint32_t a = min_nan2(min_nan2(w[0], w[1]), min_nan2(w[2], w[3])), b = max_nan2(max_nan2(w[0], w[1]), max_nan2(w[2], w[3]));
+        a = min_nan2(a, __byte_perm(a, a, 0x1032));
+        b = max_nan2(b, __byte_perm(b, b, 0x1032));
+        a = __byte_perm(a, b, 0x5410);                         // least below, largest above: both cross the lanes in one word
+#pragma unroll
+        for (int o = 4; o < 16; o <<= 1) {
+            const uint32_t y = __shfl_xor_sync(0xffffffffu, a, o);
+            a = __byte_perm(min_nan2(a, y), max_nan2(a, y), 0x7610);
+        }
+        lo = __uint_as_float(a << 16);
+        hi = __uint_as_float(a & 0xffff0000u);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+};
 __device__ __forceinline__ void store8(float *p, const float (&v)[8])
 {
     *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
@@ -166,42 +256,31 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__
     const Block blk = block_of(r, b, warp >> 1, lane);
     if (blk.m == 0 || blk.page < 0) return;
     const T *x0 = (blk.side ? v : k) + ((size_t)b * r.c.Hkv + blk.head) * r.m * D;
-    float x[W][8];
+    Eight<T> x[W];
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-        if (blk.has(j)) {
-            load8(x0 + (size_t)(blk.first + j) * D + w * kGroup + i * 8, x[w]);
-        } else {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) x[w][c] = 0.f;
-        }
+        if (blk.has(j)) x[w].load(x0 + (size_t)(blk.first + j) * D + w * kGroup + i * 8);
+        else x[w].clear();
     }
     uint8_t *base = side_base(r.c, blk.page, blk.head, blk.side);
     uint32_t *params = reinterpret_cast<uint32_t *>(base + (size_t)r.c.page_size * (D / 2));
     uint32_t codes[W], param[W];
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-        float lo = x[w][0], hi = lo;
-        uint32_t big = __float_as_uint(lo) & 0x7fffffffu;
-#pragma unroll
-        for (int c = 1; c < 8; ++c) {
-            lo = fminf(lo, x[w][c]);
-            hi = fmaxf(hi, x[w][c]);
-            big = max(big, __float_as_uint(x[w][c]) & 0x7fffffffu);
-        }
-#pragma unroll
-        for (int o = 4; o < 16; o <<= 1) {                 // the group's four lanes
-            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-            big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
-        }
+        float lo, hi;
+        x[w].range(lo, hi);
         codes[w] = 0;
-        param[w] = 0x7fc07fc0u;                            // a value that is not finite: NaN for the group
-        if (big < 0x7f800000u) {
+        param[w] = 0x7fc07fc0u;                                // a value that is not finite: NaN for the group
+        if (fmaxf(fabsf(lo), fabsf(hi)) < __int_as_float(0x7f800000) && lo == lo) {
             const uint32_t sb = scale_bits(lo, hi), zb = __float_as_uint(lo), zr = (zb + 0x7fffu + ((zb >> 16) & 1u)) & 0xffff0000u;
             const float s = __uint_as_float(sb << 16), z = __uint_as_float(zr);
             param[w] = sb | zr;
-            if (s > 0.f) codes[w] = codes_of(x[w], z, s);
+            if (s > 0.f) {
+                float v[8];
+                x[w].get(v);
+                // bf16 tensors: z is the least value itself and (hi - z) / s at most 15 (1 + 2^-8)
+                codes[w] = codes_of<sizeof(T) == 4>(v, z, s);
+            }
         }
     }
     if (blk.has(j) && i == 0) store_words(params + (size_t)(blk.at + j) * W, param);
