@@ -85,6 +85,30 @@ template <bool CLAMP> __device__ __forceinline__ uint32_t codes_of(const float (
     return codes;
 }
 
+// The same for bf16 channels, in fewer instructions.  d = x - z is exact where adding z gives x back; then a quotient corrected by its exact
+// remainder is the quotient of d and s to half an ulp: a quotient half way between two codes (one channel in 500) comes out as exactly
+// that, any other is a 2^-17th or more away from it (d has 17 bits at most, s 8), and adding 1.5 x 2^23 rounds half to even.
+__device__ __forceinline__ uint32_t codes_of_bf16(const float (&x)[8], float z, float s)
+{
+    constexpr float kWhole = 12582912.f;
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    const f2 inv2 = pack2(inv, inv), z2 = pack2(z, z), whole = pack2(kWhole, kWhole), back = pack2(-kWhole, -kWhole), minus = pack2(-z, -z), s2 = pack2(-s, -s);
+    f2 n[4];
+    uint32_t lost = 0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const f2 v = pack2(x[c], x[c + 4]), d = add2(v, minus), r = mul2(d, inv2), q = fma2(fma2(r, s2, d), inv2, r);
+        lost |= (uint32_t)(add2(d, z2) ^ v) | (uint32_t)((add2(d, z2) ^ v) >> 32);
+        n[c] = add2(add2(q, whole), back);
+    }
+    if ((lost & 0x7fffffffu) != 0 || s < 1e-30f || s > 1e30f) return codes_of<false>(x, z, s);
+    const f2 by16 = pack2(16.f, 16.f), word = add2(fma2(fma2(n[3], by16, n[2]), pack2(256.f, 256.f), fma2(n[1], by16, n[0])), pack2(8388608.f, 8388608.f));
+    float lo, hi;
+    unpack2(word, lo, hi);
+    return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410);
+}
+
 // least and largest of eight channels; NaN if one is
 __device__ __forceinline__ float min_nan(float a, float b)
 {
@@ -187,31 +211,29 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&v)[8])
 struct Rows {
     Cache4 c;
     const int32_t *start, *count;
-    int m, blocks;                         // blocks of 16 places that m tokens may touch
+    int m, shift;                          // shift: log2 of the page size where that is whole, else -1
     int *status;
 };
 
-// A warp's block of 16 places: (side, head, block) by its number within the batch row.
+// A warp's block of 16 places.
 struct Block {
-    int side, head, first, m, at, page;    // first: the call's token at the block's first place (may be negative); m tokens in all; page < 0: none
+    int first, m, at, page;                // first: the call's token at the block's first place (may be negative); m tokens in all; page < 0: none
     __device__ __forceinline__ bool has(int j) const { return first + j >= 0 && first + j < m; }
-    __device__ __forceinline__ bool any() const { return first < m && first > -kBlockTokens; }
 };
 __device__ __forceinline__ Block block_of(const Rows &r, int b, int n, int lane)
 {
     Block k;
-    const int rows = r.blocks * r.c.Hkv, x = n % rows, start = r.start[b];
-    k.side = n / rows;
-    k.head = x / r.blocks;
+    const int start = r.start[b];
     k.m = r.count != nullptr ? min(max(r.count[b], 0), r.m) : r.m;
-    const long long pos = ((long long)start >> 4) * kBlockTokens + (long long)(x % r.blocks) * kBlockTokens;
-    k.first = (int)(pos - start);
+    k.first = n * kBlockTokens - (start & 15);
     k.at = 0;
     k.page = -1;
-    if (k.side > 1 || !k.any()) { k.m = 0; return k; }
-    if (pos >= 0 && pos < (long long)r.c.max_pages * r.c.page_size) {
-        k.at = (int)pos % r.c.page_size;
-        k.page = r.c.pages[(size_t)b * r.c.max_pages + (int)pos / r.c.page_size];
+    if (k.first >= k.m) { k.m = 0; return k; }
+    const uint32_t pos = (uint32_t)start + (uint32_t)k.first;       // places before the first wrap round to beyond the last
+    if (pos < (uint32_t)(r.c.max_pages * r.c.page_size)) {
+        const uint32_t page = r.shift >= 0 ? pos >> r.shift : pos / (uint32_t)r.c.page_size;
+        k.at = (int)(pos - page * r.c.page_size);
+        k.page = r.c.pages[(size_t)b * r.c.max_pages + page];
         if (k.page >= r.c.num_pages) k.page = -1;
     }
     if (k.page < 0 && lane == 0 && r.status != nullptr) atomicOr(r.status, 32 /* LOT_DEV_PAGE */);
@@ -251,52 +273,59 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__ Rows r, const T *k, const T *v)
 {
     constexpr int W = D / kGroup;
-    const int lane = threadIdx.x & 31, b = blockIdx.y, t = lane & 3, i = (lane >> 2) & 3, e = lane >> 4;
-    const int warp = (int)(blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)), u = warp & 1, j = 8 * u + 2 * t + e;      // half a block
-    const Block blk = block_of(r, b, warp >> 1, lane);
+    const int lane = threadIdx.x & 31, b = blockIdx.z, head = blockIdx.y >> 1, side = blockIdx.y & 1, t = lane & 3, i = (lane >> 2) & 3, e = lane >> 4;
+    const Block blk = block_of(r, b, (int)(blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5)), lane);
     if (blk.m == 0 || blk.page < 0) return;
-    const T *x0 = (blk.side ? v : k) + ((size_t)b * r.c.Hkv + blk.head) * r.m * D;
-    Eight<T> x[W];
+    const T *x0 = (side ? v : k) + ((size_t)b * r.c.Hkv + head) * r.m * D + (long long)blk.first * D + i * 8;
+    Eight<T> x[2][W];
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-        if (blk.has(j)) x[w].load(x0 + (size_t)(blk.first + j) * D + w * kGroup + i * 8);
-        else x[w].clear();
-    }
-    uint8_t *base = side_base(r.c, blk.page, blk.head, blk.side);
-    uint32_t *params = reinterpret_cast<uint32_t *>(base + (size_t)r.c.page_size * (D / 2));
-    uint32_t codes[W], param[W];
+    for (int u = 0; u < 2; ++u) {
+        const int j = 8 * u + 2 * t + e;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-        float lo, hi;
-        x[w].range(lo, hi);
-        codes[w] = 0;
-        param[w] = 0x7fc07fc0u;                                // a value that is not finite: NaN for the group
-        if (fmaxf(fabsf(lo), fabsf(hi)) < __int_as_float(0x7f800000) && lo == lo) {
-            const uint32_t sb = scale_bits(lo, hi), zb = __float_as_uint(lo), zr = (zb + 0x7fffu + ((zb >> 16) & 1u)) & 0xffff0000u;
-            const float s = __uint_as_float(sb << 16), z = __uint_as_float(zr);
-            param[w] = sb | zr;
-            if (s > 0.f) {
-                float v[8];
-                x[w].get(v);
-                // bf16 tensors: z is the least value itself and (hi - z) / s at most 15 (1 + 2^-8)
-                codes[w] = codes_of<sizeof(T) == 4>(v, z, s);
-            }
+        for (int w = 0; w < W; ++w) {
+            if (blk.has(j)) x[u][w].load(x0 + j * D + w * kGroup);
+            else x[u][w].clear();
         }
     }
-    if (blk.has(j) && i == 0) store_words(params + (size_t)(blk.at + j) * W, param);
-    if (blk.side == 0) {
-        if (blk.has(j)) store_words(base + (size_t)(blk.at + j) * (D / 2) + i * 4 * W, codes);
-        return;
-    }
+    uint8_t *base = side_base(r.c, blk.page, head, side);
+    uint32_t *params = reinterpret_cast<uint32_t *>(base + (size_t)r.c.page_size * (D / 2));
 #pragma unroll
-    for (int w = 0; w < W; ++w) codes[w] = exchange(codes[w], lane);
-    uint8_t *o = base + value_half(blk.at + 8 * u + 2 * t, lane >> 2, 0, W);
-    const bool even = blk.has(8 * u + 2 * t), odd = blk.has(8 * u + 2 * t + 1);
-    if (even && odd) {
-        store_words(o, codes);
-    } else if (even || odd) {
+    for (int u = 0; u < 2; ++u) {
+        const int j = 8 * u + 2 * t + e;
+        uint32_t codes[W], param[W];
 #pragma unroll
-        for (int w = 0; w < W; ++w) *reinterpret_cast<uint16_t *>(o + 4 * w + (odd ? 2 : 0)) = (uint16_t)(odd ? codes[w] >> 16 : codes[w]);
+        for (int w = 0; w < W; ++w) {
+            float lo, hi;
+            x[u][w].range(lo, hi);
+            codes[w] = 0;
+            param[w] = 0x7fc07fc0u;                            // a value that is not finite: NaN for the group
+            if (fmaxf(fabsf(lo), fabsf(hi)) < __int_as_float(0x7f800000) && lo == lo) {
+                const uint32_t sb = scale_bits(lo, hi), zb = __float_as_uint(lo), zr = (zb + 0x7fffu + ((zb >> 16) & 1u)) & 0xffff0000u;
+                const float s = __uint_as_float(sb << 16), z = __uint_as_float(zr);
+                param[w] = sb | zr;
+                if (s > 0.f) {
+                    float y[8];
+                    x[u][w].get(y);
+                    // bf16 tensors: z is the least value itself and (hi - z) / s at most 15 (1 + 2^-8)
+                    codes[w] = sizeof(T) == 4 ? codes_of<true>(y, z, s) : codes_of_bf16(y, z, s);
+                }
+            }
+        }
+        if (blk.has(j) && i == 0) store_words(params + (size_t)(blk.at + j) * W, param);
+        if (side == 0) {
+            if (blk.has(j)) store_words(base + (size_t)(blk.at + j) * (D / 2) + i * 4 * W, codes);
+            continue;
+        }
+#pragma unroll
+        for (int w = 0; w < W; ++w) codes[w] = exchange(codes[w], lane);
+        uint8_t *o = base + value_half(blk.at + 8 * u + 2 * t, lane >> 2, 0, W);
+        const bool even = blk.has(8 * u + 2 * t), odd = blk.has(8 * u + 2 * t + 1);
+        if (even && odd) {
+            store_words(o, codes);
+        } else if (even || odd) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) *reinterpret_cast<uint16_t *>(o + 4 * w + (odd ? 2 : 0)) = (uint16_t)(odd ? codes[w] >> 16 : codes[w]);
+        }
     }
 }
 
@@ -304,8 +333,8 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ Rows r, T *k, T *v)
 {
     constexpr int W = D / kGroup;
-    const int lane = threadIdx.x & 31, b = blockIdx.y, t = lane & 3, i = (lane >> 2) & 3, e = lane >> 4;
-    const Block blk = block_of(r, b, (int)(blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)), lane);
+    const int lane = threadIdx.x & 31, b = blockIdx.z, head = blockIdx.y >> 1, side = blockIdx.y & 1, t = lane & 3, i = (lane >> 2) & 3, e = lane >> 4;
+    const Block blk = block_of(r, b, (int)(blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5)), lane);
     if (blk.m == 0) return;
     uint32_t codes[2][W], param[2][W];
 #pragma unroll
@@ -314,23 +343,23 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ 
 #pragma unroll
         for (int w = 0; w < W; ++w) codes[u][w] = param[u][w] = 0;
         if (blk.page < 0) continue;                            // a token whose page is missing reads as zeros
-        const uint8_t *base = side_base(r.c, blk.page, blk.head, blk.side);
+        const uint8_t *base = side_base(r.c, blk.page, head, side);
         load_words(reinterpret_cast<const uint32_t *>(base + (size_t)r.c.page_size * (D / 2)) + (size_t)(blk.at + j) * W, param[u]);
-        load_words(blk.side ? base + value_half(blk.at + 8 * u + 2 * t, lane >> 2, 0, W) : base + (size_t)(blk.at + j) * (D / 2) + i * 4 * W, codes[u]);
+        load_words(side ? base + value_half(blk.at + 8 * u + 2 * t, lane >> 2, 0, W) : base + (size_t)(blk.at + j) * (D / 2) + i * 4 * W, codes[u]);
     }
-    T *x0 = (blk.side ? v : k) + ((size_t)b * r.c.Hkv + blk.head) * r.m * D;
+    T *x0 = (side ? v : k) + ((size_t)b * r.c.Hkv + head) * r.m * D + (long long)blk.first * D + i * 8;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int j = 8 * u + 2 * t + e;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            if (blk.side) codes[u][w] = exchange(codes[u][w], lane);
+            if (side) codes[u][w] = exchange(codes[u][w], lane);
             if (!blk.has(j)) continue;
             const float s = param_scale(param[u][w]), z = param_least(param[u][w]);
             float x[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) x[c] = fmaf(s, (float)((codes[u][w] >> (4 * c)) & 15u), z);
-            store8(x0 + (size_t)(blk.first + j) * D + w * kGroup + i * 8, x);
+            store8(x0 + j * D + w * kGroup, x);
         }
     }
 }
@@ -340,9 +369,20 @@ template <typename F> cudaError_t by_width(int dtype, int d, F f)
     if (dtype == 0) return d == 32 ? f(float{}, std::integral_constant<int, 32>{}) : d == 64 ? f(float{}, std::integral_constant<int, 64>{}) : f(float{}, std::integral_constant<int, 128>{});
     return d == 32 ? f(__nv_bfloat16{}, std::integral_constant<int, 32>{}) : d == 64 ? f(__nv_bfloat16{}, std::integral_constant<int, 64>{}) : f(__nv_bfloat16{}, std::integral_constant<int, 128>{});
 }
-int blocks_of(int m) { return (int)(((long long)m + 2 * (kBlockTokens - 1)) / kBlockTokens); }
-// per: warps a block of places
-dim3 grid_of(const Cache4 &c, int B, int m, int per) { return dim3((unsigned)((2ll * c.Hkv * blocks_of(m) * per + kThreads / 32 - 1) / (kThreads / 32)), B); }
+// Blocks of 16 places that m tokens may touch, up to eight in a thread block.
+struct Shape {
+    dim3 grid;
+    unsigned threads;
+    int shift;
+};
+Shape shape_of(const Cache4 &c, int B, int m)
+{
+    const int blocks = (int)(((long long)m + 2 * (kBlockTokens - 1)) / kBlockTokens), warps = blocks < kThreads / 32 ? blocks : kThreads / 32;
+    int shift = -1;
+    for (int i = 4; i < 29; ++i)
+        if (c.page_size == 1 << i) shift = i;
+    return Shape{dim3((unsigned)((blocks + warps - 1) / warps), 2 * c.Hkv, B), 32u * warps, shift};
+}
 
 } // namespace
 
@@ -351,7 +391,8 @@ cudaError_t launch_write4(const Cache4 &c, const void *k, const void *v, const i
 {
     return by_width(dtype, c.d, [&](auto t, auto width) {
         using T = decltype(t);
-        write_kernel<T, decltype(width)::value><<<grid_of(c, B, m, 2), kThreads, 0, st>>>(Rows{c, start, count, m, blocks_of(m), status}, static_cast<const T *>(k), static_cast<const T *>(v));
+        const Shape s = shape_of(c, B, m);
+        write_kernel<T, decltype(width)::value><<<s.grid, s.threads, 0, st>>>(Rows{c, start, count, m, s.shift, status}, static_cast<const T *>(k), static_cast<const T *>(v));
         return cudaGetLastError();
     });
 }
@@ -360,7 +401,8 @@ cudaError_t launch_read4(const Cache4 &c, void *k, void *v, const int32_t *start
 {
     return by_width(dtype, c.d, [&](auto t, auto width) {
         using T = decltype(t);
-        read_kernel<T, decltype(width)::value><<<grid_of(c, B, m, 1), kThreads, 0, st>>>(Rows{c, start, count, m, blocks_of(m), status}, static_cast<T *>(k), static_cast<T *>(v));
+        const Shape s = shape_of(c, B, m);
+        read_kernel<T, decltype(width)::value><<<s.grid, s.threads, 0, st>>>(Rows{c, start, count, m, s.shift, status}, static_cast<T *>(k), static_cast<T *>(v));
         return cudaGetLastError();
     });
 }
