@@ -3,14 +3,17 @@
 // Bound by the bytes of the cache, if the instructions that take four-bit codes to operands can be kept below: 1.25 bytes a pair of
 // channels, so at the copy rate an SM has about 110 clocks for 16 tokens of 128 channels, keys and values.  Hence
 //   - the queries are the narrow side of the products (16 x 8 x 16: sixteen tokens by eight query rows), the codes the wide one, and one
-//     masked shift makes two entries of an operand: 0x4300 | code is the bf16 number 128 + code.  The query rows of a key head (its query
-//     heads times the new tokens) share its codes.
-//   - scale and least value never touch the codes: S = s (sum q (128 + n) - 128 sum q) + z sum q for each group of 32 channels, and
-//     sum_j p_j v_j = sum (p_j s_j) (n_j - 8) + sum p_j (z_j + 8 s_j); the latter product's weights p_j s_j are rounded to bf16, so the
-//     codes are centred for it (n - 8 is exact): the rounding counts for no more than it would on the values themselves.
-//   - float32 queries: three bf16 terms that sum to the number exactly; weights likewise.
+//     shift and mask make two entries of an operand: 0x4300 | code is the bf16 number 128 + code.  (0x6400 | code << 4 k, f16 numbers, would
+//     save two shifts of a word's three, but sums that begin at 1024 times the queries lose four digits of a score in the tensor cores.)
+//     The query rows of a key head (its query heads times the new tokens) share its codes.
+//   - scale and least value never touch the codes: S = s (sum q n) + z sum q for each group of 32 channels, and
+//     sum_j p_j v_j = sum (p_j s_j) (n_j - 8) + sum p_j (z_j + 8 s_j).  The 128 goes out of the values' sums by a product of the same weights
+//     with a constant, so that the rounding of the weights p_j s_j to bf16 counts for no more than it would on the values themselves.
+//   - (z - 128 s) sum q of all groups is two more products, the sums as three bf16 terms.
+//   - float32 queries: everything as three bf16 terms that sum to the number exactly, and centred codes.
 // A warp goes over chunks of 32 tokens by itself: its lanes fetch them with bulk copies into a ring of its own.  Running maximum and sum
-// per warp (the maximum moves only when a score passes it by 2^8), warps and blocks of a split join at the end.
+// per warp (the maximum moves only when a score passes it by 2^8), warps and blocks of a split join at the end: the blocks of few
+// sequences through a cluster's shared memory (one launch, latency), of many through memory and join_kernel.
 #include "lot_chain.cuh"
 #include "lot_sm100.cuh"
 #include "lot_window.cuh"
@@ -24,13 +27,13 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kWarps = 4, kThreads = kWarps * 32, kChunk = 32, kStages = 3, kRows = 8;
+constexpr int kWarps = 4, kThreads = kWarps * 32, kChunk = 32, kStages = 2, kRows = 8, kBlocks = 4;      // kBlocks: on an SM at once
 constexpr float kLift = 8.f;               // log2 of how far a weight may pass 1 before the reference moves
 
 template <int D> struct Lay {
     static constexpr int W = D / kGroup, CODES = kChunk * D / 2, PARAMS = kChunk * D / 8, STAGE = 2 * (CODES + PARAMS);
     static constexpr int RING = kStages * STAGE, MERGE = kRows * D * 4 + 2 * kRows * 4;      // of a warp
-    static constexpr int WARP = RING > MERGE ? RING : MERGE, TOTAL = kWarps * WARP + kWarps * kStages * 8 + 16;
+    static constexpr int WARP = RING > MERGE ? RING : MERGE, OWN = kWarps * WARP + kWarps * kStages * 8 + 16, TOTAL = OWN + (kRows * D + 2 * kRows) * 4;
 };
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
@@ -80,8 +83,9 @@ template <int TERMS> __device__ __forceinline__ void terms(float a, float b, uin
 
 struct Args {
     Attend4 a;
-    int splits, row_tiles, G;
-    float *part;                           // splits > 1: [row tile][B Hkv][split][kRows][D + 2]: sums, maximum (base 2), weight
+    int splits, each, row_tiles, G, shift; // each: chunks of a split; shift: log2 of the page size where that is whole, else -1
+    int clustered;                         // the splits are the blocks of a cluster
+    float *part;                           // else, splits > 1: [row tile][B Hkv][split][kRows][D + 2]: sums, maximum (base 2), weight
 };
 
 // chunks of 32 tokens that the rows at positions p0 .. p1 see: those of the sinks, then the window's
@@ -91,33 +95,40 @@ struct Chunks {
     __device__ __forceinline__ int at(int i) const { return i < sink ? i : first + i - sink; }
 };
 
+template <int W> __device__ __forceinline__ void words(const void *p, uint32_t (&w)[W])
+{
+    if constexpr (W == 4) {
+        const uint4 v = *static_cast<const uint4 *>(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else if constexpr (W == 2) {
+        const uint2 v = *static_cast<const uint2 *>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else {
+        w[0] = *static_cast<const uint32_t *>(p);
+    }
+}
+
 template <int D, typename T>
-__global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_constant__ Args A)
+__global__ void __launch_bounds__(kThreads, kBlocks) attend_kernel(const __grid_constant__ Args A)
 {
     extern __shared__ __align__(128) uint8_t smem[];
     using L = Lay<D>;
     constexpr int W = L::W, TERMS = sizeof(T) == 4 ? 3 : 1;
+    constexpr bool kLifted = TERMS == 1;                   // products of 128 + code, the 128 taken out of the sums
     const Attend4 &a = A.a;
     const Cache4 &c = a.cache;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int split = blockIdx.x % A.splits, tile = blockIdx.x / A.splits, hk = blockIdx.y, b = blockIdx.z;
     const int rows = A.G * a.band.nq, r0 = tile * kRows;
-    const int len = min(max(a.band.key_len[b], 0), a.band.nk), pos = len - a.band.nq;
+    const int len = min(max(a.band.key_len[b], 0), a.band.nk), p0 = len - a.band.nq, p1 = len - 1;     // positions of the first and last query
     // row r of the key head: query head hk G + r / nq, query r % nq
-    auto position = [&](int r) { return pos + r % a.band.nq; };
-    int p0 = pos, p1 = len - 1;
-    if (a.band.nq == 1) p0 = p1;
     Chunks ch;
-    {
-        const int lo = max(p0 - a.band.left, 0);
-        ch.last = p1 < 0 ? -1 : p1 / kChunk;
-        ch.first = lo / kChunk;
-        ch.sink = min((min(a.band.sinks, p1 + 1) + kChunk - 1) / kChunk, ch.first);
-        if (ch.sink < 0) ch.sink = 0;
-    }
     const int wfirst = max(p0 - a.band.left, 0);           // no row sees a token before it but the sinks
-    const int total = ch.count(), step = A.splits * kWarps, mine = split * kWarps + warp;
-    const int turns = mine < total ? (total - mine + step - 1) / step : 0;
+    ch.last = p1 < 0 ? -1 : p1 / kChunk;
+    ch.first = wfirst / kChunk;
+    ch.sink = max(min((min(a.band.sinks, p1 + 1) + kChunk - 1) / kChunk, ch.first), 0);
+    const int total = min(ch.count(), (split + 1) * A.each), mine = split * A.each + warp;      // this split's chunks, every fourth
+    const int turns = mine < total ? (total - mine + kWarps - 1) / kWarps : 0;
 
     uint8_t *ring = smem + warp * L::WARP;
     const uint32_t ring_s = smem_u32(ring), bars = smem_u32(smem) + kWarps * L::WARP + warp * kStages * 8;
@@ -128,42 +139,52 @@ __global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_consta
     fence_barrier_init();
     __syncthreads();
 
-    // A chunk's two blocks of 16 tokens may lie in different pages: lanes 0 .. 7 copy (block, codes or parameters, side).  Blocks that no row
-    // sees are not read, nor are their page entries.  Returns the blocks that came (bit k).
-    auto fetch = [&](int turn) -> uint32_t {
-        const int s = turn % kStages, tok = ch.at(mine + turn * step) * kChunk + (lane & 1) * kBlockTokens;
-        const bool want = tok <= p1 && (tok + kBlockTokens > wfirst || tok < a.band.sinks);
-        int page = -1;
-        if (want) {
-            page = __ldg(c.pages + (size_t)b * c.max_pages + tok / c.page_size);
-            if (page < 0 || page >= c.num_pages) {
-                if (a.status != nullptr && lane < 2) atomicOr(a.status, 32 /* LOT_DEV_PAGE */);
-                page = -1;
-            }
-        }
+    // A chunk's two blocks of 16 tokens may lie in different pages: lanes 0 .. 7 copy (block, side, codes or parameters).  Blocks that no row
+    // sees are not read, nor are their page entries.
+    const int blk = lane & 1, side = (lane >> 1) & 1, par = (lane >> 2) & 1;
+    const uint32_t dst0 = ring_s + side * (L::CODES + L::PARAMS) + (par ? L::CODES + blk * (L::PARAMS / 2) : blk * (L::CODES / 2));
+    const uint32_t piece = par ? L::PARAMS / 2 : L::CODES / 2;
+    const size_t page_bytes = side_bytes(c.page_size, D) * 2 * c.Hkv;
+    const uint32_t unit = par ? D / 8 : D / 2;
+    const uint8_t *lane_base = side_base(c, 0, hk, side) + (par ? (size_t)c.page_size * (D / 2) : 0);
+    const int32_t *table = c.pages + (size_t)b * c.max_pages;
+    auto token = [&](int turn) { return ch.at(mine + turn * kWarps) * kChunk + blk * kBlockTokens; };
+    auto page_of = [&](int tok) { return A.shift >= 0 ? tok >> A.shift : tok / c.page_size; };
+    auto entry = [&](int turn) -> int {                    // page of this lane's block, -1: none, -2: not there
+        if (turn >= turns) return -1;
+        const int tok = token(turn);
+        if (!(tok <= p1 && (tok + kBlockTokens > wfirst || tok < a.band.sinks))) return -1;
+        const int page = __ldg(table + page_of(tok));
+        return page >= 0 && page < c.num_pages ? page : -2;
+    };
+    auto fetch = [&](int turn, int page) -> uint32_t {     // the blocks that come (bit k)
+        const int s = turn % kStages;
         const uint32_t got = __ballot_sync(0xffffffffu, page >= 0) & 3u;
         if (lane == 0) mbar_arrive_expect_tx(bars + 8 * s, __popc(got) * (L::STAGE / 2));
         __syncwarp();
         if (lane < 8 && page >= 0) {
-            const int side = (lane >> 1) & 1, par = lane >> 2, blk = lane & 1, at = tok % c.page_size;
-            const uint8_t *base = side_base(c, page, hk, side);
-            const uint32_t dst = ring_s + s * L::STAGE + side * (L::CODES + L::PARAMS);
-            if (par == 0) bulk_load(dst + blk * (L::CODES / 2), base + (size_t)at * (D / 2), L::CODES / 2, bars + 8 * s);
-            else bulk_load(dst + L::CODES + blk * (L::PARAMS / 2), base + (size_t)c.page_size * (D / 2) + (size_t)at * (D / 8), L::PARAMS / 2, bars + 8 * s);
+            const int tok = token(turn), at = tok - page_of(tok) * c.page_size;
+            bulk_load(dst0 + s * L::STAGE, lane_base + page * page_bytes + (uint32_t)at * unit, piece, bars + 8 * s);
         }
+        if (page == -2 && lane < 2 && a.status != nullptr) atomicOr(a.status, 32 /* LOT_DEV_PAGE */);
         return got;
     };
     uint32_t present = 0;                                  // two bits a stage
+    int page[kStages];
+#pragma unroll
+    for (int s = 0; s < kStages; ++s) page[s] = entry(s);
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s)
-        if (s < turns) present |= fetch(s) << (2 * s);
+        if (s < turns) present |= fetch(s, page[s]) << (2 * s);
+    int ahead = page[kStages - 1];                         // page of the next chunk to fetch, asked for a turn before
 
     // queries: this lane's channels of query row g as B operands, and the rows' sums over each group
-    uint32_t qf[TERMS][W][2][2];
+    uint32_t qf[TERMS][W][2][2], zb[2], sb[2];
     float qsum[W][2];
     {
         const int r = r0 + g;
         const T *q = static_cast<const T *>(a.q) + (((size_t)b * a.H + hk * A.G + (r < rows ? r / a.band.nq : 0)) * a.band.nq + (r < rows ? r % a.band.nq : 0)) * D;
+        float mine_sum[W];
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             float x[8];
@@ -178,13 +199,12 @@ __global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_consta
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = 0.f;
             }
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += x[e];
+            float sum = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            qsum[w][0] = __shfl_sync(0xffffffffu, sum, 8 * t);             // of row 2 t
-            qsum[w][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);         // of row 2 t + 1
+            mine_sum[w] = sum;
+            qsum[w][0] = __shfl_sync(0xffffffffu, sum, 8 * t);                                         // of row 2 t
+            qsum[w][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);                                     // of row 2 t + 1
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 uint32_t o[TERMS];
@@ -193,6 +213,15 @@ __global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_consta
                 for (int m = 0; m < TERMS; ++m) qf[m][w][e >> 1][e & 1] = o[m];
             }
         }
+        // row g's sums as the operand of the least values: entries 0 .. 3 the first term of groups 0 .. 3, 4 .. 7 the second, 8 .. 11 the third
+        uint32_t z3[2][3];
+        terms<3>(mine_sum[0], W > 1 ? mine_sum[W > 1 ? 1 : 0] : 0.f, z3[0]);
+        terms<3>(W > 2 ? mine_sum[W > 2 ? 2 : 0] : 0.f, W > 2 ? mine_sum[W > 2 ? 3 : 0] : 0.f, z3[1]);
+        zb[0] = t == 0 ? z3[0][0] : t == 1 ? z3[1][0] : t == 2 ? z3[0][1] : z3[1][1];
+        zb[1] = t == 0 ? z3[0][2] : t == 1 ? z3[1][2] : 0u;
+        // -128 times as much, for the scales
+#pragma unroll
+        for (int e = 0; e < 2; ++e) sb[e] = pack(-128.f * __uint_as_float(zb[e] << 16), -128.f * __uint_as_float(zb[e] & 0xffff0000u));
     }
     const float scale = a.scale * kLog2e;
     float o[2 * W][4], zs[W][2], ref[2] = {neg_inf(), neg_inf()}, l[2] = {0.f, 0.f};
@@ -202,14 +231,15 @@ __global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_consta
         for (int e = 0; e < 4; ++e) o[m][e] = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w) zs[w][0] = zs[w][1] = 0.f;
-    const int prow[2] = {position(min(r0 + 2 * t, rows - 1)), position(min(r0 + 2 * t + 1, rows - 1))};
+    const int prow[2] = {p0 + min(r0 + 2 * t, rows - 1) % a.band.nq, p0 + min(r0 + 2 * t + 1, rows - 1) % a.band.nq};
 
     for (int turn = 0; turn < turns; ++turn) {
-        const int s = turn % kStages, tok0 = ch.at(mine + turn * step) * kChunk;
+        const int s = turn % kStages, tok0 = ch.at(mine + turn * kWarps) * kChunk;
         if (turn + kStages - 1 < turns) {
             const int sn = (turn + kStages - 1) % kStages;
             __syncwarp();                                  // the stage's readers are done
-            present = (present & ~(3u << (2 * sn))) | (fetch(turn + kStages - 1) << (2 * sn));
+            present = (present & ~(3u << (2 * sn))) | (fetch(turn + kStages - 1, ahead) << (2 * sn));
+            ahead = entry(turn + kStages);
         }
         if (!mbar_wait(bars + 8 * s, (turn / kStages) & 1, abort_flag, a.status != nullptr ? a.status : const_cast<int *>(abort_flag))) {
             for (int u = turn + 1; u < turns && u < turn + kStages; ++u)           // copies on their way, before the block may end
@@ -219,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_consta
         const uint32_t got = (present >> (2 * s)) & 3u;
         uint8_t *st = ring + s * L::STAGE;
         uint32_t *kp = reinterpret_cast<uint32_t *>(st + L::CODES), *vp = reinterpret_cast<uint32_t *>(st + 2 * L::CODES + L::PARAMS);
-        const bool whole = got == 3u && tok0 >= wfirst && tok0 + kChunk - 1 <= p1 && (p1 == p0 || (tok0 + kChunk - 1 <= p0 && tok0 >= p1 - a.band.left));
+        const bool whole = got == 3u && tok0 >= max(p1 - a.band.left, 0) && tok0 + kChunk - 1 <= p0;      // every row sees every token
         if (!whole) {
             // tokens that no row sees: parameters of zero, whatever is there
             const int j = tok0 + lane;
@@ -234,36 +264,67 @@ __global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_consta
         float S[2][4];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const uint32_t *k0 = reinterpret_cast<const uint32_t *>(st + (kb * 16 + g) * (D / 2) + t * 4 * W), *k1 = k0 + 8 * (D / 8);
             uint32_t ka[W], kc[W], pa[W], pc[W];
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                ka[w] = k0[w]; kc[w] = k1[w];
-                pa[w] = kp[(kb * 16 + g) * W + w]; pc[w] = kp[(kb * 16 + g + 8) * W + w];
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) S[kb][e] = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                // bf16 queries: the products' 128 is taken out beforehand; float32 ones: of the codes, 128 sums would cost five bits
-                constexpr float kOff = TERMS == 1 ? 128.f : 0.f;
-                float x[4] = {-kOff * qsum[w][0], -kOff * qsum[w][1], -kOff * qsum[w][0], -kOff * qsum[w][1]};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t f[4];
-                    f[0] = TERMS == 1 ? lifted(ka[w], 2 * h) : centred(ka[w], 2 * h);
-                    f[1] = TERMS == 1 ? lifted(kc[w], 2 * h) : centred(kc[w], 2 * h);
-                    f[2] = TERMS == 1 ? lifted(ka[w], 2 * h + 1) : centred(ka[w], 2 * h + 1);
-                    f[3] = TERMS == 1 ? lifted(kc[w], 2 * h + 1) : centred(kc[w], 2 * h + 1);
-#pragma unroll
-                    for (int m = TERMS - 1; m >= 0; --m) mma(x, f, qf[m][w][h][0], qf[m][w][h][1], x);
+            words<W>(st + (kb * 16 + g) * (D / 2) + t * 4 * W, ka);
+            words<W>(st + (kb * 16 + g + 8) * (D / 2) + t * 4 * W, kc);
+            words<W>(kp + (kb * 16 + g) * W, pa);
+            words<W>(kp + (kb * 16 + g + 8) * W, pc);
+            if (kLifted) {
+                // least values and scales: rows g, g + 8 by groups 2 (t % 2), 2 (t % 2) + 1
+                uint32_t f[4], h[4];
+                const bool up = t & 1;
+                if (W == 4) {
+                    const uint32_t a0 = up ? pa[W / 2] : pa[0], a1 = up ? pa[W - 1] : pa[W > 1], c0 = up ? pc[W / 2] : pc[0], c1 = up ? pc[W - 1] : pc[W > 1];
+                    f[0] = __byte_perm(a0, a1, 0x7632);
+                    f[1] = __byte_perm(c0, c1, 0x7632);
+                    h[0] = __byte_perm(a0, a1, 0x5410);
+                    h[1] = __byte_perm(c0, c1, 0x5410);
+                } else {
+                    const uint32_t a1 = W > 1 ? pa[W - 1] : 0u, c1 = W > 1 ? pc[W - 1] : 0u;
+                    f[0] = up ? 0u : __byte_perm(pa[0], a1, 0x7632);
+                    f[1] = up ? 0u : __byte_perm(pc[0], c1, 0x7632);
+                    h[0] = up ? 0u : __byte_perm(pa[0], a1, 0x5410);
+                    h[1] = up ? 0u : __byte_perm(pc[0], c1, 0x5410);
                 }
-                const float s0 = param_scale(pa[w]), s1 = param_scale(pc[w]);
-                const float z0 = fmaf(TERMS == 1 ? 0.f : 8.f, s0, param_least(pa[w])), z1 = fmaf(TERMS == 1 ? 0.f : 8.f, s1, param_least(pc[w]));
-                S[kb][0] = fmaf(s0, x[0], fmaf(z0, qsum[w][0], S[kb][0]));
-                S[kb][1] = fmaf(s0, x[1], fmaf(z0, qsum[w][1], S[kb][1]));
-                S[kb][2] = fmaf(s1, x[2], fmaf(z1, qsum[w][0], S[kb][2]));
-                S[kb][3] = fmaf(s1, x[3], fmaf(z1, qsum[w][1], S[kb][3]));
+                f[2] = f[0];
+                f[3] = f[1];
+                h[2] = h[0];
+                h[3] = h[1];
+                const float none[4] = {0.f, 0.f, 0.f, 0.f};
+                mma(S[kb], f, zb[0], zb[1], none);
+                mma(S[kb], h, sb[0], sb[1], S[kb]);
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    float x[4];
+                    const uint32_t lo[4] = {lifted(ka[w], 0), lifted(kc[w], 0), lifted(ka[w], 1), lifted(kc[w], 1)};
+                    mma(x, lo, qf[0][w][0][0], qf[0][w][0][1], none);
+                    const uint32_t hi[4] = {lifted(ka[w], 2), lifted(kc[w], 2), lifted(ka[w], 3), lifted(kc[w], 3)};
+                    mma(x, hi, qf[0][w][1][0], qf[0][w][1][1], x);
+                    const float s0 = param_scale(pa[w]), s1 = param_scale(pc[w]);
+                    S[kb][0] = fmaf(s0, x[0], S[kb][0]);
+                    S[kb][1] = fmaf(s0, x[1], S[kb][1]);
+                    S[kb][2] = fmaf(s1, x[2], S[kb][2]);
+                    S[kb][3] = fmaf(s1, x[3], S[kb][3]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) S[kb][e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t f[4] = {centred(ka[w], 2 * h), centred(kc[w], 2 * h), centred(ka[w], 2 * h + 1), centred(kc[w], 2 * h + 1)};
+#pragma unroll
+                        for (int m = TERMS - 1; m >= 0; --m) mma(x, f, qf[m][w][h][0], qf[m][w][h][1], x);
+                    }
+                    const float s0 = param_scale(pa[w]), s1 = param_scale(pc[w]);
+                    const float z0 = fmaf(8.f, s0, param_least(pa[w])), z1 = fmaf(8.f, s1, param_least(pc[w]));
+                    S[kb][0] = fmaf(s0, x[0], fmaf(z0, qsum[w][0], S[kb][0]));
+                    S[kb][1] = fmaf(s0, x[1], fmaf(z0, qsum[w][1], S[kb][1]));
+                    S[kb][2] = fmaf(s1, x[2], fmaf(z1, qsum[w][0], S[kb][2]));
+                    S[kb][3] = fmaf(s1, x[3], fmaf(z1, qsum[w][1], S[kb][3]));
+                }
             }
         }
         if (!whole) {
@@ -276,9 +337,7 @@ __global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_consta
                     S[kb][e] = seen ? S[kb][e] : neg_inf();
                 }
         }
-        float top[2];
-#pragma unroll
-        for (int q = 0; q < 2; ++q) top[q] = scale * fmaxf(fmaxf(S[0][q], S[0][q + 2]), fmaxf(S[1][q], S[1][q + 2]));
+        const float top[2] = {scale * fmaxf(fmaxf(S[0][0], S[0][2]), fmaxf(S[1][0], S[1][2])), scale * fmaxf(fmaxf(S[0][1], S[0][3]), fmaxf(S[1][1], S[1][3]))};
         if (__any_sync(0xffffffffu, top[0] > ref[0] + kLift || top[1] > ref[1] + kLift)) {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
@@ -304,14 +363,12 @@ __global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_consta
             S[kb][3] = ex2(fmaf(S[kb][3], scale, -r1v));
             l[0] += S[kb][0] + S[kb][2];
             l[1] += S[kb][1] + S[kb][3];
-            const uint8_t *vb = st + L::CODES + L::PARAMS + kb * (L::CODES / 2);
-            const uint32_t *v0 = reinterpret_cast<const uint32_t *>(vb) + lane * W, *v1 = v0 + 32 * W;
+            const uint8_t *vb = st + L::CODES + L::PARAMS + kb * (L::CODES / 2) + lane * 4 * W;
             uint32_t va[W], vc[W], pa[W], pc[W];
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                va[w] = v0[w]; vc[w] = v1[w];
-                pa[w] = vp[(kb * 16 + g) * W + w]; pc[w] = vp[(kb * 16 + g + 8) * W + w];
-            }
+            words<W>(vb, va);
+            words<W>(vb + 128 * W, vc);
+            words<W>(vp + (kb * 16 + g) * W, pa);
+            words<W>(vp + (kb * 16 + g + 8) * W, pc);
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const float s0 = param_scale(pa[w]), s1 = param_scale(pc[w]);
@@ -325,13 +382,16 @@ __global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_consta
                 for (int m = 0; m < TERMS; ++m) { x0[m] = flip(x0[m]); x1[m] = flip(x1[m]); }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    uint32_t f[4];
-                    f[0] = centred(va[w], 2 * h);
-                    f[1] = centred(va[w], 2 * h + 1);
-                    f[2] = centred(vc[w], 2 * h);
-                    f[3] = centred(vc[w], 2 * h + 1);
+                    if (kLifted) {
+                        const uint32_t f[4] = {lifted(va[w], 2 * h), lifted(va[w], 2 * h + 1), lifted(vc[w], 2 * h), lifted(vc[w], 2 * h + 1)};
+                        const uint32_t away[4] = {0xc308c308u, 0xc308c308u, 0xc308c308u, 0xc308c308u};            // -136
+                        mma(o[2 * w + h], away, x0[0], x1[0], o[2 * w + h]);
+                        mma(o[2 * w + h], f, x0[0], x1[0], o[2 * w + h]);
+                    } else {
+                        const uint32_t f[4] = {centred(va[w], 2 * h), centred(va[w], 2 * h + 1), centred(vc[w], 2 * h), centred(vc[w], 2 * h + 1)};
 #pragma unroll
-                    for (int m = TERMS - 1; m >= 0; --m) mma(o[2 * w + h], f, x0[m], x1[m], o[2 * w + h]);
+                        for (int m = TERMS - 1; m >= 0; --m) mma(o[2 * w + h], f, x0[m], x1[m], o[2 * w + h]);
+                    }
                 }
             }
         }
@@ -356,31 +416,75 @@ __global__ void __launch_bounds__(kThreads, 3) attend_kernel(const __grid_consta
         mm[kRows + 2 * t] = l[0]; mm[kRows + 2 * t + 1] = l[1];
     }
     __syncthreads();
+    const float nan = __int_as_float(0x7fc00000);
     const bool failed = *abort_flag != 0;
-    for (int idx = tid; idx < kRows * D; idx += kThreads) {
-        const int r = idx / D, ch_ = idx % D;
-        if (r0 + r >= rows) break;
-        float top = neg_inf();
+    // one row and channel of this block's warps: maximum, weight, sum
+    auto of_block = [&](int r, int col, float &top, float &sum, float &x) {
+        top = neg_inf();
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) top = fmaxf(top, reinterpret_cast<const float *>(smem + w * L::WARP)[kRows * D + r]);
         const float at = top == neg_inf() ? 0.f : top;
-        float sum = 0.f, x = 0.f;
+        sum = x = 0.f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             const float *p = reinterpret_cast<const float *>(smem + w * L::WARP);
             const float f = ex2(p[kRows * D + r] - at);
             sum += f * p[kRows * D + kRows + r];
-            x += f * p[r * D + ch_];
+            x += f * p[r * D + col];
         }
-        if (failed) sum = x = __int_as_float(0x7fc00000);
-        if (A.splits > 1) {
-            float *part = A.part + ((((size_t)tile * a.B + b) * c.Hkv + hk) * A.splits + split) * (kRows * (D + 2)) + r * (D + 2);
-            part[ch_] = x;
-            if (ch_ == 0) { part[D] = top; part[D + 1] = sum; }
-        } else {
-            const size_t row = ((size_t)b * a.H + hk * A.G + (r0 + r) / a.band.nq) * a.band.nq + (r0 + r) % a.band.nq;
-            Elem<T>::store(static_cast<T *>(a.out) + row * D + ch_, sum > 0.f ? x / sum : failed ? x : 0.f);
-            if (ch_ == 0 && a.lse != nullptr) a.lse[row] = sum > 0.f ? top * kLn2 + logf(sum) : failed ? x : neg_inf();
+        if (failed) sum = x = nan;
+    };
+    auto write = [&](int r, int col, float top, float sum, float x) {
+        const size_t row = ((size_t)b * a.H + hk * A.G + (r0 + r) / a.band.nq) * a.band.nq + (r0 + r) % a.band.nq;
+        const bool nothing = sum == 0.f;
+        Elem<T>::store(static_cast<T *>(a.out) + row * D + col, nothing ? 0.f : x / sum);
+        if (col == 0 && a.lse != nullptr) a.lse[row] = nothing ? neg_inf() : top * kLn2 + logf(sum);
+    };
+    if (A.clustered) {
+        // every block leaves its rows in its own shared memory (behind the warps' parts) and takes every splits-th number of all blocks'
+        float *own = reinterpret_cast<float *>(smem + L::OWN);
+        for (int idx = tid; idx < kRows * D; idx += kThreads) {
+            float top, sum, x;
+            of_block(idx / D, idx % D, top, sum, x);
+            own[idx] = x;
+            if (idx % D == 0) { own[kRows * D + idx / D] = top; own[kRows * D + kRows + idx / D] = sum; }
+        }
+        asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+        const uint32_t base = smem_u32(own);
+        auto of = [&](int rank, int at) {
+            uint32_t addr;
+            float v;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(base + 4u * at), "r"(rank));
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+            return v;
+        };
+        for (int idx = split * kThreads + tid; idx < kRows * D; idx += A.splits * kThreads) {
+            const int r = idx / D;
+            if (r0 + r >= rows) break;
+            float top = neg_inf(), sum = 0.f, x = 0.f;
+            for (int k = 0; k < A.splits; ++k) top = fmaxf(top, of(k, kRows * D + r));
+            const float at = top == neg_inf() ? 0.f : top;
+            for (int k = 0; k < A.splits; ++k) {
+                const float f = ex2(of(k, kRows * D + r) - at);
+                sum += f * of(k, kRows * D + kRows + r);
+                x += f * of(k, idx);
+            }
+            write(r, idx % D, top, sum, x);
+        }
+        asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");      // no block ends while another reads it
+    } else {
+        for (int idx = tid; idx < kRows * D; idx += kThreads) {
+            const int r = idx / D, col = idx % D;
+            if (r0 + r >= rows) break;
+            float top, sum, x;
+            of_block(r, col, top, sum, x);
+            if (A.splits > 1) {
+                float *part = A.part + ((((size_t)tile * a.B + b) * c.Hkv + hk) * A.splits + split) * (kRows * (D + 2)) + r * (D + 2);
+                part[col] = x;
+                if (col == 0) { part[D] = top; part[D + 1] = sum; }
+            } else {
+                write(r, col, top, sum, x);
+            }
         }
     }
     chain_next();
@@ -410,13 +514,33 @@ __global__ void __launch_bounds__(D) join_kernel(const __grid_constant__ Args A)
     if (ch == 0 && a.lse != nullptr) a.lse[row] = nothing ? neg_inf() : top * kLn2 + logf(sum);
 }
 
-// Splits of a sequence's chunks: enough blocks for two waves of three an SM, and no warp with less than two chunks.
-int splits_of(int sms, int B, int Hkv, int tiles, int nk, int nq, int left, int sinks)
+// How a sequence's chunks are split.  The lengths are on the device, so a split is a number of chunks, counted for the longest sequence there may be; a
+// shorter one leaves its last splits nothing to do.  A round is a chunk for each of a block's four warps.  Few sequences: up to eight splits of
+// up to eight rounds, the blocks of a cluster.  Else so many that the blocks fill the SMs four times over, which evens out sequences of different
+// lengths, but none of less than four rounds (a block's beginning and end cost as much as two).
+struct Split {
+    int splits, each, clustered;
+};
+Split split_of(int sms, int B, int Hkv, int tiles, int nk, int nq, int left, int sinks)
 {
-    const long long seen = (left < nk ? left + 1ll : nk) + nq - 1 + sinks, chunks = ((seen < nk ? seen : nk) + kChunk - 1) / kChunk + 1;
-    const long long blocks = (long long)B * Hkv * tiles, want = (6ll * sms + blocks - 1) / blocks, most = (chunks + 2 * kWarps - 1) / (2 * kWarps);
-    const long long s = want < most ? want : most;
-    return s < 1 ? 1 : s > 512 ? 512 : (int)s;
+    // chunks that left + nq tokens in a row may touch, and those of the sinks; never more than there are
+    const long long all = ((long long)nk + kChunk - 1) / kChunk, touched = ((long long)(left < nk ? left : nk) + nq + 2 * (kChunk - 1)) / kChunk + (sinks + kChunk - 1) / kChunk;
+    const long long chunks = touched < all ? touched : all;
+    const long long blocks = (long long)B * Hkv * tiles, rounds = (chunks + kWarps - 1) / kWarps;
+    Split s{1, (int)rounds * kWarps, 0};
+    if (rounds <= 1) return s;
+    const long long at_once = (long long)kBlocks * sms;
+    if (blocks * 2 <= at_once) {                            // a cluster may have eight blocks; a longer sequence takes more than that pays
+        const long long room = at_once / blocks, n = rounds < room ? rounds : room, m = n < 8 ? n : 8, per = (rounds + m - 1) / m;
+        if (per <= 8) return Split{(int)((rounds + per - 1) / per), (int)per * kWarps, 1};
+    }
+    const long long n = (4 * at_once + blocks - 1) / blocks;
+    long long per = (rounds + n - 1) / n;
+    if (per < 4) per = 4;
+    if ((rounds + per - 1) / per > 512) per = (rounds + 511) / 512;
+    s.splits = (int)((rounds + per - 1) / per);
+    s.each = (int)per * kWarps;
+    return s;
 }
 
 template <int D, typename T> cudaError_t run(const Args &A, cudaStream_t st)
@@ -433,7 +557,9 @@ template <int D, typename T> cudaError_t run(const Args &A, cudaStream_t st)
             set[dev] = true;
         }
     }
-    attend_kernel<D, T><<<dim3(A.splits * A.row_tiles, A.a.cache.Hkv, A.a.B), kThreads, Lay<D>::TOTAL, st>>>(A);
+    const dim3 grid(A.splits * A.row_tiles, A.a.cache.Hkv, A.a.B);
+    if (A.clustered) return cluster_launch(attend_kernel<D, T>, grid, kThreads, Lay<D>::TOTAL, A.splits, st, A);
+    attend_kernel<D, T><<<grid, kThreads, Lay<D>::TOTAL, st>>>(A);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || A.splits == 1) return e;
     return chain_launch(join_kernel<D, T>, dim3(A.G * A.a.band.nq, A.a.cache.Hkv, A.a.B), D, 0, st, A);
@@ -444,9 +570,10 @@ template <int D, typename T> cudaError_t run(const Args &A, cudaStream_t st)
 size_t attend4_workspace(int dtype, int B, int H, int Hkv, int nq, int d, int nk, int left, int sinks)
 {
     (void)dtype;
-    const int tiles = (H / Hkv * nq + kRows - 1) / kRows, s = splits_of(device_sm_count(), B, Hkv, tiles, nk, nq, left, sinks);
-    if (s == 1) return 0;
-    return ((size_t)tiles * B * Hkv * s * kRows * (d + 2) * 4 + 255) & ~(size_t)255;
+    const int tiles = (H / Hkv * nq + kRows - 1) / kRows;
+    const Split s = split_of(device_sm_count(), B, Hkv, tiles, nk, nq, left, sinks);
+    if (s.splits == 1 || s.clustered) return 0;
+    return ((size_t)tiles * B * Hkv * s.splits * kRows * (d + 2) * 4 + 255) & ~(size_t)255;
 }
 
 cudaError_t launch_attend4(const Attend4 &a, cudaStream_t st)
@@ -455,7 +582,13 @@ cudaError_t launch_attend4(const Attend4 &a, cudaStream_t st)
     A.a = a;
     A.G = a.H / a.cache.Hkv;
     A.row_tiles = (A.G * a.band.nq + kRows - 1) / kRows;
-    A.splits = splits_of(device_sm_count(), a.B, a.cache.Hkv, A.row_tiles, a.band.nk, a.band.nq, a.band.left, a.band.sinks);
+    const Split s = split_of(device_sm_count(), a.B, a.cache.Hkv, A.row_tiles, a.band.nk, a.band.nq, a.band.left, a.band.sinks);
+    A.splits = s.splits;
+    A.each = s.each;
+    A.clustered = s.clustered;
+    A.shift = -1;
+    for (int i = 4; i < 29; ++i)
+        if (a.cache.page_size == 1 << i) A.shift = i;
     A.part = static_cast<float *>(a.ws);
     const int d = a.cache.d;
     if (a.dtype == 0) return d == 32 ? run<32, float>(A, st) : d == 64 ? run<64, float>(A, st) : run<128, float>(A, st);
