@@ -1,13 +1,15 @@
 // Window attention forward of bf16 tensors on tcgen05.
 //
 // A persistent block per SM goes through items of two 128-query tiles that read the same keys: two query heads of a key head, or two
-// neighbouring tiles of one head.  Five roles: two groups of four softmax warps (one a query tile, a thread a row), one warp that loads
-// tiles (TMA), one that issues the products.  For each 128-key tile
+// neighbouring tiles of one head.  Four roles: two groups of eight softmax warps (one a query tile; a warp 16 rows, whose 128 columns lie in lane quads),
+// one warp that loads tiles (TMA), one that issues the products.  For each 128-key tile
 //   S = Q K^T in tensor memory -> the group's rows: maximum, exponentials, sum -> P (bf16) back into tensor memory, where it is the first
 //   operand of O += P V -> O stays in tensor memory over the item's tiles.
 // The running maximum moves only when a score passes it by 2^8 (weights up to 2^8 lose nothing in float32 sums or bf16 weights), so O is
-// hardly ever rescaled.  While one group takes exponentials the products of the other run.
-// Key tiles outside a block's window are never visited, 32-column parts outside a warp's never worked on.
+// hardly ever rescaled, and the quads' maxima need not be joined to see that nothing passes it.
+// Bound by the exponentials (16 a clock and SM: 2048 clocks for both tiles) and, at 128 channels, as much by the products.  With eight softmax warps (a thread a
+// row) a warp's waits, loads and loop around 2000 clocks of exponentials took as long again: two warps a scheduler did not hide them.
+// Key tiles outside a block's window are never visited, 64-column halves outside a warp's never worked on.
 #include "lot_chain.cuh"
 #include "lot_window_tc.cuh"
 
@@ -17,7 +19,7 @@ namespace lot {
 namespace window {
 namespace {
 
-constexpr int kThreads = 320, kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kThreads = 576, kMmaWarp = 16, kLoadWarp = 17, kGroup8 = 256;
 constexpr float kLift = 8.f;
 
 template <int DP> struct Plan {
@@ -26,14 +28,15 @@ template <int DP> struct Plan {
     static constexpr int kQ = 0, kKV = kQStages * 2 * kTileBytes<DP>, kBars = kKV + kSlots * kTileBytes<DP>;
     // q_full, q_empty [stages]; kv_full, kv_empty [slots]; s_full, s_free, p_full, o_done [2]
     static constexpr int bQFull = kBars, bQEmpty = bQFull + 8 * kQStages, bFull = bQEmpty + 8 * kQStages, bEmpty = bFull + 8 * kSlots, bS = bEmpty + 8 * kSlots,
-                         bSFree = bS + 16, bP = bSFree + 16, bO = bP + 16, kAbort = bO + 16, kTmem = kAbort + 8, kTotal = kTmem + 8;
+                         bSFree = bS + 16, bP = bSFree + 16, bO = bP + 16, kAbort = bO + 16, kTmem = kAbort + 8, kInv = kTmem + 8, kTotal = kInv + 2 * kTile * 4;
     static constexpr int cS = 0, cP = kApart ? 128 : 0, cO = kApart ? 192 : 128, kCols = 256;      // columns of a tile's half of tensor memory
 };
 
 struct Args {
     Fwd a;
     CUtensorMap q, k, v;
-    int G, paired, tiles, per_tile, items;                 // paired: two heads of a key head; tiles: query tiles of a head
+    int paired, steps, items;                              // paired: two heads of a key head; steps: items of a head or pair
+    FastDiv per, heads, group;                             // items of a step; heads or pairs of a batch row; query heads of a key head
 };
 
 struct Item {
@@ -42,19 +45,21 @@ struct Item {
     KeyTiles keys;
     __device__ __forceinline__ int head(int t) const { return h0 + (t ? hstep : 0); }
     __device__ __forceinline__ int row(int t) const { return row0 + (t ? rstep : 0); }
+    // the last key tile first: with right = 0 every row has seen its own key after it, so that the maximum is near its place from the start
+    __device__ __forceinline__ int tile(int n) const { return keys.at(keys.n - 1 - n); }
 };
 __device__ __forceinline__ Item item_of(const Args &A, int i)
 {
     Item it;
     // last query tiles first: with a window that is not limited to the left they are the longest
-    const int per = A.per_tile, t = (A.paired ? A.tiles : (A.tiles + 1) / 2) - 1 - i / per, x = i % per, heads = A.paired ? A.a.H / 2 : A.a.H;
-    it.b = x / heads;
-    const int y = x % heads;
+    int x, y;
+    const int t = A.steps - 1 - A.per.divmod(i, x);
+    it.b = A.heads.divmod(x, y);
     it.h0 = A.paired ? 2 * y : y;
     it.hstep = A.paired ? 1 : 0;
     it.row0 = A.paired ? t * kTile : 2 * t * kTile;
     it.rstep = A.paired ? 0 : kTile;
-    it.hk = it.h0 / A.G;
+    it.hk = A.group.div(it.h0);
     it.R = row_of(A.a.band, it.b);
     it.keys = key_tiles(it.R, it.R.pos + it.row0, it.R.pos + min(it.row0 + it.rstep + kTile, A.a.band.nq) - 1);
     return it;
@@ -104,8 +109,8 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
         for (int s = 0; s < P::kSlots; ++s) { mbar_init(sbase + P::bFull + 8 * s, 1); mbar_init(sbase + P::bEmpty + 8 * s, 1); }
         for (int t = 0; t < 2; ++t) {
             mbar_init(sbase + P::bS + 8 * t, 1);
-            mbar_init(sbase + P::bSFree + 8 * t, 4);
-            mbar_init(sbase + P::bP + 8 * t, 4);
+            mbar_init(sbase + P::bSFree + 8 * t, 8);
+            mbar_init(sbase + P::bP + 8 * t, 8);
             mbar_init(sbase + P::bO + 8 * t, 1);
         }
         abort_flag[0] = abort_flag[1] = 0;
@@ -122,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
         uint32_t n = 0;                                    // tiles loaded, keys and values counted apart
         bool ok = true;
         for (w.begin(A); ok && w.more(A); w.next(A)) {
-            const int j0 = w.it.keys.at(w.tile) * kTile, kv = w.it.b * A.a.Hkv + w.it.hk;
+            const int j0 = w.it.tile(w.tile) * kTile, kv = w.it.b * A.a.Hkv + w.it.hk;
             if (w.tile == 0) {
                 const int s = w.count % P::kQStages;
                 const uint32_t turn = w.count / P::kQStages;
@@ -177,21 +182,20 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
         for (; ok && w.more(A); w.next(A), ++g) {
             const bool follow = ahead.more(A);
             const uint32_t vs = (2 * g + 1) % P::kSlots;
-            if (P::kApart && follow) {
-                ok = operands(g + 1);
-                for (int t = 0; ok && t < 2; ++t) {
+            ok = !follow || !P::kApart || operands(g + 1);
+            for (int t = 0; ok && t < 2; ++t) {
+                if (P::kApart && follow) {
                     ok = wait(sbase + P::bSFree + 8 * t, g);
                     if (!ok) break;
                     tc_fence_after();
                     scores(g + 1, t);
                 }
-                if (!ok) break;
-            }
-            ok = wait(sbase + P::bFull + 8 * vs, (2 * g + 1) / P::kSlots);
-            if (!ok) break;
-            const int j0 = w.it.keys.at(w.tile) * kTile;
-            if (!all_used(w.it.R, j0)) clear_unused<DP>(smem + P::kKV + vs * TB, w.it.R, j0, lane);
-            for (int t = 0; t < 2; ++t) {
+                if (t == 0) {
+                    ok = wait(sbase + P::bFull + 8 * vs, (2 * g + 1) / P::kSlots);
+                    if (!ok) break;
+                    const int j0 = w.it.tile(w.tile) * kTile;
+                    if (!all_used(w.it.R, j0)) clear_unused<DP>(smem + P::kKV + vs * TB, w.it.R, j0, lane);
+                }
                 ok = wait(sbase + P::bP + 8 * t, g);
                 if (!ok) break;
                 tc_fence_after();
@@ -207,138 +211,170 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
                     scores(g + 1, t);
                 }
             }
+            if (!ok) break;
             if (follow) ahead.next(A);
         }
         if (*abort_flag) {                                 // products on their way end before tensor memory is given back
             for (int x = 0; x < 4096; ++x) (void)mbar_try_wait(sbase + P::bO, (g & 1) ^ 1);
         }
     } else {
-        const int t = warp >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * P::kCols;
+        const int t = warp >> 3, half = (warp >> 2) & 1, first = (warp & 3) * 32 + half * 16, quad = lane & 3;
+        // a warp's 16 rows as lanes of tensor memory; this thread has rows first + lane / 4 (A) and 8 further (B), columns 8 i + 2 quad, + 1
+        const uint32_t rows16 = tmem + ((uint32_t)first << 16) + t * P::kCols, rows32 = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * P::kCols;
+        float *inv = reinterpret_cast<float *>(smem + P::kInv) + t * kTile;
         const float c = A.a.scale * kLog2e;
+        const f2 c2 = pack2(c, c);
         uint32_t g = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < A.items; i += gridDim.x) {
             const Item it = item_of(A, i);
             const Row &R = it.R;
-            const int q = it.row(t) + row, p = R.pos + q, pw0 = R.pos + it.row(t) + (warp & 3) * 32, pw1 = pw0 + 31;
-            float m = neg_inf(), l = 0.f;
+            const int q0 = it.row(t), pw0 = R.pos + q0 + first, pw1 = pw0 + 15, pa = pw0 + (lane >> 2), pb = pa + 8;
+            const int full_hi = R.hi(pw0), any_hi = R.hi(pw1), full_lo = pw1 - R.left, any_lo = pw0 - R.left;
+            float ma = neg_inf(), mb = neg_inf(), la = 0.f, lb = 0.f;
             for (int n = 0; ok && n < it.keys.n; ++n, ++g) {
-                const int j0 = it.keys.at(n) * kTile;
-                float s[2][32];                            // S is read twice, 32 columns at a time, the next ones on their way
-                int kind[4];                               // of 32 columns, for the warp: 0 nothing seen, 1 a part, 2 all
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int a = j0 + 32 * k, b = a + 31;
-                    kind[k] = a > R.hi(pw1) || (b < pw0 - R.left && a >= R.sinks) ? 0 : b <= R.hi(pw0) && (a >= pw1 - R.left || b < R.sinks) ? 2 : 1;
-                }
+                const int j0 = it.tile(n) * kTile;
+                float x[2][32];
                 ok = wait(sbase + P::bS + 8 * t, g);
                 if (!ok) break;
                 tc_fence_after();
-                float top = neg_inf();
-                tmem_ld32(lanes + P::cS, s[0]);
+                tile::tmem_ld_acc<8>(rows16 + P::cS, x[0]);
+                tile::tmem_ld_acc<8>(rows16 + P::cS + 64, x[1]);
+                settle(x[0]);
+                settle(x[1]);
+                if (P::kApart) {                           // S may be written again
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(sbase + P::bSFree + 8 * t);
+                }
+                int kind[2];                               // of 64 columns, for the warp: 0 nothing seen, 1 a part, 2 all
+                float ta = neg_inf(), tb = neg_inf();
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float (&x)[32] = s[k & 1];
-                    settle(x);
-                    tmem_ld32(lanes + P::cS + 32 * ((k + 1) & 3), s[(k + 1) & 1]);
+                for (int k = 0; k < 2; ++k) {
+                    const int a = j0 + 64 * k, b = a + 63;
+                    kind[k] = a > any_hi || (b < any_lo && a >= R.sinks) ? 0 : b <= full_hi && (a >= full_lo || b < R.sinks) ? 2 : 1;
                     if (kind[k] == 0) continue;
                     if (kind[k] == 1) {
-                        const uint32_t seen = seen_keys(R, p, j0 + 32 * k);
+                        const int base = a + 2 * quad, ha = R.hi(pa) - base, hb = R.hi(pb) - base, fa = pa - R.left - base, fb = fa + 8, ns = R.sinks - base;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[e] = (seen >> e) & 1u ? x[e] : neg_inf();
+                        for (int e = 0; e < 32; ++e) {
+                            const int col = 8 * (e >> 2) + (e & 1);
+                            const bool seen = e & 2 ? col <= hb && (col >= fb || col < ns) : col <= ha && (col >= fa || col < ns);
+                            x[k][e] = seen ? x[k][e] : neg_inf();
+                        }
                     }
-                    float y[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-                    for (int e = 4; e < 32; ++e) y[e & 3] = fmaxf(y[e & 3], x[e]);
-                    top = fmaxf(top, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+                    for (int e = 0; e < 32; e += 4) {
+                        ta = tile::max3(ta, x[k][e], x[k][e + 1]);
+                        tb = tile::max3(tb, x[k][e + 2], x[k][e + 3]);
+                    }
                 }
-                top *= c;
-                const bool lift = __any_sync(0xffffffffu, top > m + kLift);
-                float f = 1.f;
+                ta *= c;
+                tb *= c;
+                float fa = 1.f, fb = 1.f;
+                const bool lift = __any_sync(0xffffffffu, ta > ma + kLift || tb > mb + kLift);
                 if (lift) {
-                    const float to = fmaxf(m, top);
-                    f = to == neg_inf() ? 1.f : ex2(m - to);
-                    l *= f;
-                    m = to;
+                    ta = fmaxf(ta, __shfl_xor_sync(0xffffffffu, ta, 1));
+                    tb = fmaxf(tb, __shfl_xor_sync(0xffffffffu, tb, 1));
+                    ta = fmaxf(ma, fmaxf(ta, __shfl_xor_sync(0xffffffffu, ta, 2)));
+                    tb = fmaxf(mb, fmaxf(tb, __shfl_xor_sync(0xffffffffu, tb, 2)));
+                    fa = ta == neg_inf() ? 1.f : ex2(ma - ta);
+                    fb = tb == neg_inf() ? 1.f : ex2(mb - tb);
+                    ma = ta;
+                    mb = tb;
+                    la *= fa;
+                    lb *= fb;
                 }
-                const float ref = m == neg_inf() ? 0.f : m;
+                const float ra = ma == neg_inf() ? 0.f : -ma, rb = mb == neg_inf() ? 0.f : -mb;
+                const f2 ra2 = pack2(ra, ra), rb2 = pack2(rb, rb);
+                f2 sa = pack2(la, 0.f), sb = pack2(lb, 0.f);
+                uint32_t w[2][16];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if (kind[k] == 0) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[k][e] = 0u;
+                        continue;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        float u, v;
+                        unpack2(fma2(pack2(x[k][e], x[k][e + 1]), c2, ra2), u, v);
+                        u = ex2(u);
+                        v = ex2(v);
+                        sa = add2(sa, pack2(u, v));
+                        w[k][e / 2] = tile::pack_bf16(u, v);
+                        unpack2(fma2(pack2(x[k][e + 2], x[k][e + 3]), c2, rb2), u, v);
+                        u = ex2(u);
+                        v = ex2(v);
+                        sb = add2(sb, pack2(u, v));
+                        w[k][e / 2 + 1] = tile::pack_bf16(u, v);
+                    }
+                }
+                {
+                    float u, v;
+                    unpack2(sa, u, v);
+                    la = u + v;
+                    unpack2(sb, u, v);
+                    lb = u + v;
+                }
                 if (g > 0) {                               // P is free, O may be touched
                     ok = wait(sbase + P::bO + 8 * t, g - 1);
                     if (!ok) break;
                     tc_fence_after();
                 }
+                tile::tmem_st_pk<8>(rows16 + P::cP, w[0]);
+                tile::tmem_st_pk<8>(rows16 + P::cP + 32, w[1]);
                 if (lift && n > 0) {
-                    settle(s[0]);
+#pragma unroll 1
+                    for (int k = 0; k < DP; k += 32) {
+                        uint32_t o[16];
+                        tile::tmem_ld_pk<8>(rows16 + P::cO + k, o);
+                        tmem_wait_ld();
 #pragma unroll
-                    for (int k = 0; k < DP / 32; ++k) {
-                        tmem_ld32(lanes + P::cO + 32 * k, s[1]);
-                        settle(s[1]);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) s[1][e] *= f;
-                        tmem_st32(lanes + P::cO + 32 * k, reinterpret_cast<const uint32_t *>(s[1]));
+                        for (int e = 0; e < 16; ++e) asm volatile("mul.f32 %0, %0, %1;" : "+r"(o[e]) : "f"(e & 1 ? fb : fa));
+                        tile::tmem_st_pk<8>(rows16 + P::cO + k, o);
                     }
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float (&x)[32] = s[k & 1];
-                    settle(x);
-                    if (k < 3) tmem_ld32(lanes + P::cS + 32 * (k + 1), s[(k + 1) & 1]);
-                    else if (P::kApart) {                  // all of S has been read
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(sbase + P::bSFree + 8 * t);
-                    }
-                    uint32_t w[16];
-                    if (kind[k] == 0) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = 0u;
-                    } else {
-                        if (kind[k] == 1) {
-                            const uint32_t seen = seen_keys(R, p, j0 + 32 * k);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = (seen >> e) & 1u ? x[e] : neg_inf();
-                        }
-                        float sum[2] = {0.f, 0.f};
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            x[e] = ex2(fmaf(x[e], c, -ref));
-                            sum[e & 1] += x[e];
-                        }
-                        l += sum[0] + sum[1];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = tile::pack_bf16(x[2 * e], x[2 * e + 1]);
-                    }
-                    tmem_st16(lanes + P::cP + 16 * k, w);
                 }
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(sbase + P::bP + 8 * t);
             }
-            if (ok && it.keys.n > 0) {
-                ok = wait(sbase + P::bO + 8 * t, g - 1);
+            // the rows' weights for whoever reads them: a warp takes all 32 rows of its lanes of tensor memory and half of the channels
+            const int q = q0 + (warp & 3) * 32 + lane;
+            const size_t head = ((size_t)it.b * A.a.H + it.head(t)) * A.a.band.nq;
+            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(A.a.out) + (head + q) * A.a.d;
+            if (it.keys.n > 0) {
+                if (ok) ok = wait(sbase + P::bO + 8 * t, g - 1);
                 tc_fence_after();
-            }
-            const float inv = !ok ? __int_as_float(0x7fc00000) : l > 0.f ? 1.f / l : 0.f;
-            const bool there = q < A.a.band.nq;
-            const size_t at = ((size_t)it.b * A.a.H + it.head(t)) * A.a.band.nq + q;
-#pragma unroll
-            for (int k = 0; k < DP / 32; ++k) {
-                float o[32];
-                if (it.keys.n > 0) {
-                    tmem_ld32(lanes + P::cO + 32 * k, o);
-                    settle(o);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                const float nan = __int_as_float(0x7fc00000);
+                la += __shfl_xor_sync(0xffffffffu, la, 1);
+                lb += __shfl_xor_sync(0xffffffffu, lb, 1);
+                la += __shfl_xor_sync(0xffffffffu, la, 2);
+                lb += __shfl_xor_sync(0xffffffffu, lb, 2);
+                if (quad < 2) {
+                    const int r = first + (lane >> 2) + 8 * quad;
+                    const float l = quad ? lb : la, m = quad ? mb : ma;
+                    inv[r] = !ok ? nan : l == 0.f ? 0.f : 1.f / l;
+                    if (A.a.lse != nullptr && q0 + r < A.a.band.nq) A.a.lse[head + q0 + r] = !ok ? nan : l == 0.f ? neg_inf() : m * kLn2 + logf(l);
                 }
-                // a row that sees nothing: its sums are zero
+                named_bar_sync(1 + t, kGroup8);
+                const float f = inv[(warp & 3) * 32 + lane];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] *= inv;
-                if (there) store_row32(static_cast<__nv_bfloat16 *>(A.a.out) + at * A.a.d, 32 * k, A.a.d, o);
+                for (int k = half * (DP / 2); k < half * (DP / 2) + DP / 2; k += 32) {
+                    float o[32];
+                    tmem_ld32(rows32 + P::cO + k, o);
+                    settle(o);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = f == 0.f ? 0.f : o[e] * f;
+                    if (q < A.a.band.nq) store_row32(out, k, A.a.d, o);
+                }
+            } else if (q < A.a.band.nq) {
+                const float o[32] = {};
+                for (int k = half * (DP / 2); k < half * (DP / 2) + DP / 2; k += 32) store_row32(out, k, A.a.d, o);
+                if (half == 0 && A.a.lse != nullptr) A.a.lse[head + q] = neg_inf();
             }
-            if (there && A.a.lse != nullptr) A.a.lse[at] = !ok ? inv : l > 0.f ? m * kLn2 + logf(l) : neg_inf();
         }
     }
     tc_fence_before();
@@ -390,11 +426,14 @@ cudaError_t launch_fwd_tc(const Fwd &a, cudaStream_t st)
 {
     Args A;
     A.a = a;
-    A.G = a.H / a.Hkv;
-    A.paired = A.G % 2 == 0;
-    A.tiles = (a.band.nq + kTile - 1) / kTile;
-    A.per_tile = a.B * (A.paired ? a.H / 2 : a.H);
-    A.items = (A.paired ? A.tiles : (A.tiles + 1) / 2) * A.per_tile;
+    const int G = a.H / a.Hkv, tiles = (a.band.nq + kTile - 1) / kTile;
+    A.paired = G % 2 == 0;
+    A.steps = A.paired ? tiles : (tiles + 1) / 2;
+    const int heads = A.paired ? a.H / 2 : a.H;
+    A.items = A.steps * a.B * heads;
+    A.per = fast_div(a.B * heads);
+    A.heads = fast_div(heads);
+    A.group = fast_div(G);
     if (!make_tile_map(&A.q, a.q, (long long)a.B * a.H, a.band.nq, a.d)) return cudaErrorInvalidValue;
     A.k = A.v = A.q;                                       // without keys no item has tiles
     if (a.band.nk > 0 && (!make_tile_map(&A.k, a.k, (long long)a.B * a.Hkv, a.band.nk, a.d) ||

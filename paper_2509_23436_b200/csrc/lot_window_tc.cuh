@@ -140,6 +140,27 @@ __device__ __forceinline__ void store_row32(__nv_bfloat16 *row, int col, int d, 
                                                                     tile::pack_bf16(v[c + 4], v[c + 5]), tile::pack_bf16(v[c + 6], v[c + 7]));
 }
 
+// Division of numbers below 2^31 by a number fixed at the launch: q = (n + high half of n mul) >> shift.
+struct FastDiv {
+    uint32_t mul, shift, by;
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+    __device__ __forceinline__ int divmod(int n, int &rest) const
+    {
+        const int q = div(n);
+        rest = n - q * (int)by;
+        return q;
+    }
+};
+inline FastDiv fast_div(int d)
+{
+    FastDiv f;
+    f.by = (uint32_t)d;
+    f.shift = 0;
+    while ((1ull << f.shift) < (uint64_t)d) ++f.shift;
+    f.mul = (uint32_t)(((1ull << 32) * ((1ull << f.shift) - (uint64_t)d)) / (uint64_t)d + 1);
+    return f;
+}
+
 // ---- barriers -------------------------------------------------------------------------------------------------------------
 struct Waits {                             // bounded waits of one block: the first that gives up ends them all
     volatile int *abort_flag;
