@@ -1,8 +1,9 @@
 // Window attention forward of bf16 tensors on tcgen05.
 //
 // A persistent block per SM goes through items of two 128-query tiles that read the same keys: two query heads of a key head, or two
-// neighbouring tiles of one head.  Four roles: two groups of eight softmax warps (one a query tile; a warp 16 rows, whose 128 columns lie in lane quads),
-// one warp that loads tiles (TMA), one that issues the products.  For each 128-key tile
+// neighbouring tiles of one head.  Roles: two groups of eight softmax warps (one a query tile; a warp 16 rows, whose 128 columns lie in lane quads),
+// for each group a warp that issues its products (one for both was busy all the time), a warp that loads tiles (TMA) and one that clears
+// values no query sees.  For each 128-key tile
 //   S = Q K^T in tensor memory -> the group's rows: maximum, exponentials, sum -> P (bf16) back into tensor memory, where it is the first
 //   operand of O += P V -> O stays in tensor memory over the item's tiles.
 // The running maximum moves only when a score passes it by 2^8 (weights up to 2^8 lose nothing in float32 sums or bf16 weights), so O is
@@ -19,16 +20,16 @@ namespace lot {
 namespace window {
 namespace {
 
-constexpr int kThreads = 576, kMmaWarp = 16, kLoadWarp = 17, kGroup8 = 256;
+constexpr int kThreads = 640, kMmaWarp = 16, kLoadWarp = 18, kClearWarp = 19, kGroup8 = 256;
 constexpr float kLift = 8.f;
 
 template <int DP> struct Plan {
     static constexpr bool kApart = DP == 64;               // P has columns of its own: the next S may be written while P is made
     static constexpr int kQStages = DP == 64 ? 2 : 1, kSlots = DP == 64 ? 8 : 4;
     static constexpr int kQ = 0, kKV = kQStages * 2 * kTileBytes<DP>, kBars = kKV + kSlots * kTileBytes<DP>;
-    // q_full, q_empty [stages]; kv_full, kv_empty [slots]; s_full, s_free, p_full, o_done [2]
+    // q_full, q_empty [stages]; kv_full, kv_empty [slots]; s_full, s_free, p_full, o_done [2]; clear [slots]
     static constexpr int bQFull = kBars, bQEmpty = bQFull + 8 * kQStages, bFull = bQEmpty + 8 * kQStages, bEmpty = bFull + 8 * kSlots, bS = bEmpty + 8 * kSlots,
-                         bSFree = bS + 16, bP = bSFree + 16, bO = bP + 16, kAbort = bO + 16, kTmem = kAbort + 8, kInv = kTmem + 8, kTotal = kInv + 2 * kTile * 4;
+                         bSFree = bS + 16, bP = bSFree + 16, bO = bP + 16, bClear = bO + 16, kAbort = bClear + 8 * kSlots, kTmem = kAbort + 8, kInv = kTmem + 8, kTotal = kInv + 2 * kTile * 4;
     static constexpr int cS = 0, cP = kApart ? 128 : 0, cO = kApart ? 192 : 128, kCols = 256;      // columns of a tile's half of tensor memory
 };
 
@@ -45,7 +46,7 @@ struct Item {
     KeyTiles keys;
     __device__ __forceinline__ int head(int t) const { return h0 + (t ? hstep : 0); }
     __device__ __forceinline__ int row(int t) const { return row0 + (t ? rstep : 0); }
-    // the last key tile first: with right = 0 every row has seen its own key after it, so that the maximum is near its place from the start
+    // the last key tile first: with right = 0 every row sees its own key in it, so that the maximum is near its place from the start
     __device__ __forceinline__ int tile(int n) const { return keys.at(keys.n - 1 - n); }
 };
 __device__ __forceinline__ Item item_of(const Args &A, int i)
@@ -94,6 +95,13 @@ struct Walk {
     }
 };
 
+// how many of the columns 0, 1, 8, 9, 16, 17, .. 57 a quad's thread has lie before column n
+__device__ __forceinline__ int columns(int n)
+{
+    n = min(max(n, 0), 64);
+    return 2 * (n >> 3) + min(n & 7, 2);
+}
+
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_constant__ Args A)
 {
@@ -105,8 +113,8 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + P::kAbort);
     const Waits wait{abort_flag, A.a.status != nullptr ? A.a.status : reinterpret_cast<int *>(smem + P::kAbort + 4)};
     if (tid == 0) {
-        for (int s = 0; s < P::kQStages; ++s) { mbar_init(sbase + P::bQFull + 8 * s, 1); mbar_init(sbase + P::bQEmpty + 8 * s, 1); }
-        for (int s = 0; s < P::kSlots; ++s) { mbar_init(sbase + P::bFull + 8 * s, 1); mbar_init(sbase + P::bEmpty + 8 * s, 1); }
+        for (int s = 0; s < P::kQStages; ++s) { mbar_init(sbase + P::bQFull + 8 * s, 1); mbar_init(sbase + P::bQEmpty + 8 * s, 2); }
+        for (int s = 0; s < P::kSlots; ++s) { mbar_init(sbase + P::bFull + 8 * s, 1); mbar_init(sbase + P::bEmpty + 8 * s, 3); mbar_init(sbase + P::bClear + 8 * s, 1); }
         for (int t = 0; t < 2; ++t) {
             mbar_init(sbase + P::bS + 8 * t, 1);
             mbar_init(sbase + P::bSFree + 8 * t, 8);
@@ -120,7 +128,12 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(smem + P::kTmem);
+    // all columns are this block's, so they begin at 0, which the products' addresses take for granted
+    constexpr uint32_t tmem = 0;
+    if (tid == 0 && *reinterpret_cast<volatile uint32_t *>(smem + P::kTmem) != tmem) {
+        *abort_flag = 1;
+        atomicOr(wait.status, 4 /* LOT_DEV_TIMEOUT */);
+    }
 
     if (warp == kLoadWarp) {
         Walk w;
@@ -153,69 +166,75 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
             for (uint32_t u = n > P::kSlots ? n - P::kSlots : 0; u < n; ++u)
                 for (int x = 0; x < 4096 && !mbar_try_wait(sbase + P::bFull + 8 * (u % P::kSlots), (u / P::kSlots) & 1); ++x) {}
         }
-    } else if (warp == kMmaWarp) {
+    } else if (warp == kClearWarp) {
+        // Values that no query of the batch row sees are multiplied by weights of zero: they must be numbers.  This warp passes every tile in turn and
+        // gives its slot free like the products' warps, so that none of its waits is a whole turn ahead or behind.
+        Walk w;
+        uint32_t n = 0;
+        bool ok = true;
+        for (w.begin(A); ok && w.more(A); w.next(A)) {
+            const int j0 = w.it.tile(w.tile) * kTile;
+            for (int side = 0; ok && side < 2; ++side, ++n) {
+                const uint32_t s = n % P::kSlots;
+                ok = wait(sbase + P::bFull + 8 * s, n / P::kSlots);
+                if (!ok) break;
+                if (side && !all_used(w.it.R, j0)) {
+                    clear_unused<DP>(smem + P::kKV + s * TB, w.it.R, j0, lane);
+                    if (lane == 0) mbar_arrive(sbase + P::bClear + 8 * s);
+                }
+                if (lane == 0) mbar_arrive(sbase + P::bEmpty + 8 * s);
+            }
+        }
+    } else if (warp >= kMmaWarp) {
+        const int t = warp - kMmaWarp;
+        const uint32_t leader = elect_one();
         Walk w, ahead;
         w.begin(A);
         ahead = w;
-        uint32_t g = 0;                                    // tiles done
-        bool ok = true;
-        // S of the tile `ahead` stands at, its place among this block's tiles `at`
-        auto scores = [&](uint32_t at, int t) {
-            if (elect_one()) {
-                product_rows<DP>(tmem + t * P::kCols + P::cS, sbase + P::kQ + (2 * (ahead.count % P::kQStages) + t) * TB, sbase + P::kKV + (2 * at % P::kSlots) * TB);
-                umma_commit(sbase + P::bS + 8 * t);
-                if (t == 1) {
-                    umma_commit(sbase + P::bEmpty + 8 * (2 * at % P::kSlots));
-                    if (ahead.tile == ahead.it.keys.n - 1) umma_commit(sbase + P::bQEmpty + 8 * (ahead.count % P::kQStages));
-                }
-            }
-            __syncwarp();
+        uint32_t g = 0, cleared = 0;                       // tiles done; for each slot, whether its values were cleared an odd number of times
+        // S of the tile `ahead` stands at, number `at` of this block's: its queries and keys have come
+        auto scores = [&](uint32_t at) {
+            const uint32_t s = 2 * at % P::kSlots, q = ahead.count % P::kQStages;
+            if (ahead.tile == 0 && !wait(sbase + P::bQFull + 8 * q, ahead.count / P::kQStages)) return false;
+            if (!wait(sbase + P::bFull + 8 * s, 2 * at / P::kSlots)) return false;
+            product_rows<DP>(leader, tmem + t * P::kCols + P::cS, sbase + P::kQ + (2 * q + t) * TB, sbase + P::kKV + s * TB);
+            commit_to(leader, sbase + P::bS + 8 * t);
+            commit_to(leader, sbase + P::bEmpty + 8 * s);
+            if (ahead.tile == ahead.it.keys.n - 1) commit_to(leader, sbase + P::bQEmpty + 8 * q);
+            return true;
         };
-        auto operands = [&](uint32_t at) {                 // its queries and keys have come
-            if (ahead.tile == 0 && !wait(sbase + P::bQFull + 8 * (ahead.count % P::kQStages), ahead.count / P::kQStages)) return false;
-            return wait(sbase + P::bFull + 8 * (2 * at % P::kSlots), 2 * at / P::kSlots);
-        };
-        if (w.more(A)) {
-            ok = operands(0);
-            if (ok) { scores(0, 0); scores(0, 1); ahead.next(A); }
-        }
+        bool ok = !w.more(A) || scores(0);
+        if (w.more(A)) ahead.next(A);
         for (; ok && w.more(A); w.next(A), ++g) {
             const bool follow = ahead.more(A);
             const uint32_t vs = (2 * g + 1) % P::kSlots;
-            ok = !follow || !P::kApart || operands(g + 1);
-            for (int t = 0; ok && t < 2; ++t) {
-                if (P::kApart && follow) {
-                    ok = wait(sbase + P::bSFree + 8 * t, g);
-                    if (!ok) break;
-                    tc_fence_after();
-                    scores(g + 1, t);
-                }
-                if (t == 0) {
-                    ok = wait(sbase + P::bFull + 8 * vs, (2 * g + 1) / P::kSlots);
-                    if (!ok) break;
-                    const int j0 = w.it.tile(w.tile) * kTile;
-                    if (!all_used(w.it.R, j0)) clear_unused<DP>(smem + P::kKV + vs * TB, w.it.R, j0, lane);
-                }
-                ok = wait(sbase + P::bP + 8 * t, g);
+            if (P::kApart && follow) {
+                ok = wait(sbase + P::bSFree + 8 * t, g);
                 if (!ok) break;
                 tc_fence_after();
-                if (elect_one()) {
-                    product_weights<DP>(tmem + t * P::kCols + P::cO, tmem + t * P::kCols + P::cP, sbase + P::kKV + vs * TB, w.tile > 0);
-                    umma_commit(sbase + P::bO + 8 * t);
-                    if (t == 1) umma_commit(sbase + P::bEmpty + 8 * vs);
-                }
-                __syncwarp();
-                if (!P::kApart && follow) {
-                    if (t == 0) ok = operands(g + 1);
-                    if (!ok) break;
-                    scores(g + 1, t);
-                }
+                ok = scores(g + 1);
+                if (!ok) break;
             }
+            ok = wait(sbase + P::bFull + 8 * vs, (2 * g + 1) / P::kSlots);
             if (!ok) break;
-            if (follow) ahead.next(A);
+            if (!all_used(w.it.R, w.it.tile(w.tile) * kTile)) {
+                ok = wait(sbase + P::bClear + 8 * vs, cleared >> vs);
+                if (!ok) break;
+                cleared ^= 1u << vs;
+            }
+            ok = wait(sbase + P::bP + 8 * t, g);
+            if (!ok) break;
+            tc_fence_after();
+            product_weights<DP, 1>(leader, tmem + t * P::kCols + P::cO, tmem + t * P::kCols + P::cP, sbase + P::kKV + vs * TB, w.tile > 0);
+            commit_to(leader, sbase + P::bO + 8 * t);
+            commit_to(leader, sbase + P::bEmpty + 8 * vs);
+            if (follow) {
+                if (!P::kApart && !(ok = scores(g + 1))) break;
+                ahead.next(A);
+            }
         }
         if (*abort_flag) {                                 // products on their way end before tensor memory is given back
-            for (int x = 0; x < 4096; ++x) (void)mbar_try_wait(sbase + P::bO, (g & 1) ^ 1);
+            for (int x = 0; x < 4096; ++x) (void)mbar_try_wait(sbase + P::bO + 8 * t, (g & 1) ^ 1);
         }
     } else {
         const int t = warp >> 3, half = (warp >> 2) & 1, first = (warp & 3) * 32 + half * 16, quad = lane & 3;
@@ -227,13 +246,19 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
         uint32_t g = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < A.items; i += gridDim.x) {
-            const Item it = item_of(A, i);
-            const Row &R = it.R;
-            const int q0 = it.row(t), pw0 = R.pos + q0 + first, pw1 = pw0 + 15, pa = pw0 + (lane >> 2), pb = pa + 8;
-            const int full_hi = R.hi(pw0), any_hi = R.hi(pw1), full_lo = pw1 - R.left, any_lo = pw0 - R.left;
+            // what the loop needs of the item, and no more: registers
+            int n_tiles, sink, first_tile, ha, la_, hb, lb_, ns, full_hi, any_hi, full_lo, any_lo;
+            {
+                const Item it = item_of(A, i);
+                const Row &R = it.R;
+                const int pw0 = R.pos + it.row(t) + first, pw1 = pw0 + 15, pa = pw0 + (lane >> 2), pb = pa + 8;
+                n_tiles = it.keys.n; sink = it.keys.sink; first_tile = it.keys.first;
+                ha = R.hi(pa) - 2 * quad; la_ = pa - R.left - 2 * quad; hb = R.hi(pb) - 2 * quad; lb_ = pb - R.left - 2 * quad; ns = R.sinks - 2 * quad;
+                full_hi = R.hi(pw0); any_hi = R.hi(pw1); full_lo = pw1 - R.left; any_lo = pw0 - R.left;
+            }
             float ma = neg_inf(), mb = neg_inf(), la = 0.f, lb = 0.f;
-            for (int n = 0; ok && n < it.keys.n; ++n, ++g) {
-                const int j0 = it.tile(n) * kTile;
+            for (int n = n_tiles - 1; ok && n >= 0; --n, ++g) {             // last key tile first
+                const int j0 = (n < sink ? n : first_tile + n - sink) * kTile;
                 float x[2][32];
                 ok = wait(sbase + P::bS + 8 * t, g);
                 if (!ok) break;
@@ -252,15 +277,17 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int a = j0 + 64 * k, b = a + 63;
-                    kind[k] = a > any_hi || (b < any_lo && a >= R.sinks) ? 0 : b <= full_hi && (a >= full_lo || b < R.sinks) ? 2 : 1;
+                    kind[k] = a > any_hi || (b < any_lo && a - 2 * quad >= ns) ? 0 : b <= full_hi && (a >= full_lo || b - 2 * quad < ns) ? 2 : 1;
                     if (kind[k] == 0) continue;
                     if (kind[k] == 1) {
-                        const int base = a + 2 * quad, ha = R.hi(pa) - base, hb = R.hi(pb) - base, fa = pa - R.left - base, fb = fa + 8, ns = R.sinks - base;
+                        // a row's sixteen columns of the half as bits
+                        const int to_a = columns(ha - a + 1), to_b = columns(hb - a + 1), s = columns(ns - a);
+                        const uint32_t sa = ((1u << to_a) - 1u) & (~((1u << columns(la_ - a)) - 1u) | ((1u << s) - 1u));
+                        const uint32_t sb = ((1u << to_b) - 1u) & (~((1u << columns(lb_ - a)) - 1u) | ((1u << s) - 1u));
 #pragma unroll
                         for (int e = 0; e < 32; ++e) {
-                            const int col = 8 * (e >> 2) + (e & 1);
-                            const bool seen = e & 2 ? col <= hb && (col >= fb || col < ns) : col <= ha && (col >= fa || col < ns);
-                            x[k][e] = seen ? x[k][e] : neg_inf();
+                            const int bit = 2 * (e >> 2) + (e & 1);
+                            x[k][e] = ((e & 2 ? sb : sa) >> bit) & 1u ? x[k][e] : neg_inf();
                         }
                     }
 #pragma unroll
@@ -325,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
                 }
                 tile::tmem_st_pk<8>(rows16 + P::cP, w[0]);
                 tile::tmem_st_pk<8>(rows16 + P::cP + 32, w[1]);
-                if (lift && n > 0) {
+                if (lift && n < n_tiles - 1) {
 #pragma unroll 1
                     for (int k = 0; k < DP; k += 32) {
                         uint32_t o[16];
@@ -342,7 +369,10 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
                 if (lane == 0) mbar_arrive(sbase + P::bP + 8 * t);
             }
             // the rows' weights for whoever reads them: a warp takes all 32 rows of its lanes of tensor memory and half of the channels
-            const int q = q0 + (warp & 3) * 32 + lane;
+            int again = i;
+            asm volatile("" : "+r"(again));                // not kept over the loop
+            const Item it = item_of(A, again);
+            const int q0 = it.row(t), q = q0 + (warp & 3) * 32 + lane;
             const size_t head = ((size_t)it.b * A.a.H + it.head(t)) * A.a.band.nq;
             __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(A.a.out) + (head + q) * A.a.d;
             if (it.keys.n > 0) {
@@ -368,11 +398,11 @@ __global__ void __launch_bounds__(kThreads, 1) fwd_tc_kernel(const __grid_consta
                     settle(o);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = f == 0.f ? 0.f : o[e] * f;
-                    if (q < A.a.band.nq) store_row32(out, k, A.a.d, o);
+                    if (q < A.a.band.nq) store_row(out, k, A.a.d, o);
                 }
             } else if (q < A.a.band.nq) {
                 const float o[32] = {};
-                for (int k = half * (DP / 2); k < half * (DP / 2) + DP / 2; k += 32) store_row32(out, k, A.a.d, o);
+                for (int k = half * (DP / 2); k < half * (DP / 2) + DP / 2; k += 32) store_row(out, k, A.a.d, o);
                 if (half == 0 && A.a.lse != nullptr) A.a.lse[head + q] = neg_inf();
             }
         }

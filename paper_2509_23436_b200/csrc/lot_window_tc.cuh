@@ -73,33 +73,58 @@ template <int DP> __device__ __forceinline__ void clear_unused(uint8_t *tile, co
 }
 __device__ __forceinline__ bool all_used(const Row &R, int j0) { return R.used(j0) && j0 + kTile <= R.len && (j0 >= R.first || j0 + kTile <= R.sinks); }
 
-// ---- products, issued by one thread -----------------------------------------------------------------------------------
-// D (tensor memory, 128 x N) = or += A (tensor memory, 128 x 16 bf16: two to a column) B
-__device__ __forceinline__ void umma_bf16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+// ---- products ---------------------------------------------------------------------------------------------------------------
+// The whole warp computes the descriptors, so that they stay in uniform registers; the lane with `leader` set issues (one fixed lane: a branch around
+// the products, and addresses in ordinary registers, made the issue of eight products take twice as long as the products).
+// D (tensor memory, 128 x N) = or += A B; descriptors as low word (address) and high word
+__device__ __forceinline__ void issue_ss(uint32_t leader, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\t"
-                 "setp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\t"
+                 "setp.ne.b32 p, %5, 0;\n\t"
+                 "setp.ne.b32 q, %6, 0;\n\t"
+                 "mov.b64 a, {%1, %3};\n\t"
+                 "mov.b64 b, {%2, %3};\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}"
+                 ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
 }
-// D = X Y^T over DP channels, both tiles with 64 channels a panel row; N rows of Y
-template <int DP, int N = kTile> __device__ __forceinline__ void product_rows(uint32_t d, uint32_t x, uint32_t y)
+// A (tensor memory, 128 x 16 bf16: two to a column)
+__device__ __forceinline__ void issue_ts(uint32_t leader, uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate)
 {
-    constexpr uint32_t idesc = make_idesc_bf16(128, N, 0, 0);
-    const uint64_t dx = make_smem_desc(x, 16, 1024), dy = make_smem_desc(y, 16, 1024);
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 b;\n\t"
+                 "setp.ne.b32 p, %5, 0;\n\t"
+                 "setp.ne.b32 q, %6, 0;\n\t"
+                 "mov.b64 b, {%2, %3};\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void commit_to(uint32_t leader, uint32_t bar)
+{
+    asm volatile("{\n\t.reg .pred q;\n\t"
+                 "setp.ne.b32 q, %1, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader) : "memory");
+}
+// descriptor words (make_smem_desc): rows of 64 channels, K-major; and the same rows as the K of an MN-major operand, panels of 64 channels apart
+constexpr uint32_t kDescRows = (1024u >> 4) | (1u << 14) | (2u << 29), kDescRowsLo = (16u >> 4) << 16, kDescColsLo = ((kTile * 128u) >> 4) << 16;
+// D = X Y^T over DP channels, both tiles with 64 channels a panel row
+template <int DP> __device__ __forceinline__ void product_rows(uint32_t leader, uint32_t d, uint32_t x, uint32_t y)
+{
+    constexpr uint32_t idesc = make_idesc_bf16(128, kTile, 0, 0);
+    const uint32_t lx = (x >> 4) | kDescRowsLo, ly = (y >> 4) | kDescRowsLo;
 #pragma unroll
     for (int ks = 0; ks < DP / 16; ++ks) {
         const uint32_t off = (ks >> 2) * (kTile * 128 / 16) + (ks & 3) * 2;
-        umma_bf16(d, dx + off, dy + off, idesc, ks != 0);
+        issue_ss(leader, d, lx + off, ly + off, kDescRows, idesc, ks != 0);
     }
 }
-// D (128 x DP) += W Y: W 128 x 128 bf16 in tensor memory, Y's 128 rows
-template <int DP> __device__ __forceinline__ void product_weights(uint32_t d, uint32_t w, uint32_t y, bool accumulate)
+// D (128 x DP) += W Y: W 128 x 128 bf16 in tensor memory, 64 / PARTS neighbouring columns at w, w + 32, .. each; Y's 128 rows
+template <int DP, int PARTS> __device__ __forceinline__ void product_weights(uint32_t leader, uint32_t d, uint32_t w, uint32_t y, bool accumulate)
 {
     constexpr uint32_t idesc = make_idesc_bf16(128, DP, 0, 1);
-    const uint64_t dy = make_smem_desc(y, kTile * 128, 1024);
+    constexpr int RUN = kTile / 16 / PARTS;                // products to a part
+    const uint32_t ly = (y >> 4) | kDescColsLo;
 #pragma unroll
-    for (int ks = 0; ks < kTile / 16; ++ks) umma_bf16_ts(d, w + ks * 8, dy + ks * 128, idesc, accumulate || ks != 0);
+    for (int ks = 0; ks < kTile / 16; ++ks)
+        issue_ts(leader, d, w + ks / RUN * 32 + ks % RUN * 8, ly + ks * 128, kDescRows, idesc, accumulate || ks != 0);
 }
 
 // ---- tensor memory ------------------------------------------------------------------------------------------------------
@@ -130,11 +155,11 @@ __device__ __forceinline__ void settle(float (&v)[32])
                    "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])::"memory");
 }
 
-// 32 numbers of one row as bf16 to columns col .. col + 31 of a [rows][d] tensor; d is a multiple of 8
-__device__ __forceinline__ void store_row32(__nv_bfloat16 *row, int col, int d, const float (&v)[32])
+// N numbers of one row as bf16 to columns col .. col + N - 1 of a [rows][d] tensor; d is a multiple of 8
+template <int N> __device__ __forceinline__ void store_row(__nv_bfloat16 *row, int col, int d, const float (&v)[N])
 {
 #pragma unroll
-    for (int c = 0; c < 32; c += 8)
+    for (int c = 0; c < N; c += 8)
         if (col + c < d)
             *reinterpret_cast<uint4 *>(row + col + c) = make_uint4(tile::pack_bf16(v[c], v[c + 1]), tile::pack_bf16(v[c + 2], v[c + 3]),
                                                                     tile::pack_bf16(v[c + 4], v[c + 5]), tile::pack_bf16(v[c + 6], v[c + 7]));

@@ -8,9 +8,10 @@
 // (seven products of a pair of tiles where one pass with sums shared by atomics or in memory takes five; with a window those sums would be
 // written and read once for every key tile, several times what the two products cost).  Both kinds are the same loop: a standing pair of
 // tiles X1, X2, a stream of pairs Y1, Y2, S = X1 Y1^T, dP = X2 Y2^T, weights as first operand from tensor memory: [+= P Y2], += dS Y1.
-// Eight warps make the weights (a thread: a row, half the columns), one loads, one issues the products.  P takes the columns of S that its
-// own warps have read, dS those of dP, so the products of one and the exponentials of the other run side by side:
-//   products   P Y2 (i), S (i+1) | dS Y1 (i), dP (i+1) | ..        weights   dS (i)         | P (i+1)          | ..
+// Sixteen warps make the weights (a thread: a row, a quarter of the columns), one loads, one clears keys that no query sees, two issue the
+// products.  P takes the columns of S that its own warps have read, dS those of dP, so the products of one and the exponentials of the other
+// run side by side:
+//   products   P Y2 (i), S (i+1) by one warp | dS Y1 (i), dP (i+1) by the other | ..        weights   dS (i)  | P (i+1)  | ..
 // A key tile whose list is long (sinks: every later query; few key heads) is cut into parts of a fixed length, whose float32 sums
 // merge_kernel adds in order.
 #include "lot_chain.cuh"
@@ -22,14 +23,14 @@ namespace lot {
 namespace window {
 namespace {
 
-constexpr int kThreads = 320, kMmaWarp = 8, kLoadWarp = 9;
-constexpr float kNever = 1e30f;            // lse2 of rows that see nothing or do not exist: their weights are zero
+constexpr int kThreads = 640, kMmaWarp = 16, kLoadWarp = 18, kClearWarp = 19;
+constexpr float kNever = -1e30f;           // -lse2 of rows that see nothing or do not exist: their weights are zero
 
 template <int DP> struct Plan {
     static constexpr int kXStages = DP == 64 ? 2 : 1, kYStages = DP == 64 ? 4 : 2, kStat = 2 * kTile * 4;
     static constexpr int kX = 0, kY = kXStages * 2 * kTileBytes<DP>, kYBytes = 2 * kTileBytes<DP>, kS = kY + kYStages * kYBytes, kBars = kS + kYStages * kStat;
     static constexpr int bXFull = kBars, bXEmpty = bXFull + 8 * kXStages, bYFull = bXEmpty + 8 * kXStages, bYEmpty = bYFull + 8 * kYStages,
-                         bS = bYEmpty + 8 * kYStages, bDP = bS + 8, bW1 = bDP + 8, bW2 = bW1 + 8, bAcc = bW2 + 8, kAbort = bAcc + 8, kTmem = kAbort + 8,
+                         bS = bYEmpty + 8 * kYStages, bDP = bS + 8, bW1 = bDP + 8, bW2 = bW1 + 8, bAcc = bW2 + 8, bClear = bAcc + 8, kAbort = bClear + 8 * kYStages, kTmem = kAbort + 8,
                          kTotal = kTmem + 8;
     static constexpr int cS = 0, cDP = 128, cV = 256, cK = 256 + DP;
 };
@@ -37,9 +38,10 @@ template <int DP> struct Plan {
 struct Args {
     Bwd a;
     CUtensorMap q, k, v, dout;
-    const float *stat;                     // [B H][query tiles][2][128]: lse2, D
+    const float *stat;                     // [B H][query tiles][2][128]: -lse2, -D
     float *part;                           // parts of key tiles: [part][2][128][DP]
     int G, qtiles, ktiles, sink_tiles;     // of a head
+    FastDiv kheads, qheads, Hkv, H, group, sink_cut, key_cut;      // heads of all batch rows, of one; query heads of a key head; parts of a tile
     int sink_parts, key_parts;             // parts of a key tile with and without sinks
     int sink_items, key_items, items;      // sink tiles' parts first, then the other key tiles', then the queries
 };
@@ -58,10 +60,10 @@ __device__ __forceinline__ Item item_of(const Args &A, int i)
     if (i < A.sink_items + A.key_items) {
         it.keys = true;
         const bool sink = i < A.sink_items;
-        const int parts = sink ? A.sink_parts : A.key_parts, y = sink ? i : i - A.sink_items, heads = A.a.B * A.a.Hkv, p = y % parts, x = y / parts;
-        const int kt = (sink ? 0 : A.sink_tiles) + x / heads;
-        it.b = x % heads / A.a.Hkv;
-        it.h = x % heads % A.a.Hkv;
+        const int parts = sink ? A.sink_parts : A.key_parts, y = sink ? i : i - A.sink_items;
+        int p, z;
+        const int x = sink ? A.sink_cut.divmod(y, p) : A.key_cut.divmod(y, p), kt = (sink ? 0 : A.sink_tiles) + A.kheads.divmod(x, z);
+        it.b = A.Hkv.divmod(z, it.h);
         it.x0 = kt * kTile;
         it.part = parts == 1 ? -1 : sink || A.sink_parts == 1 ? y : A.sink_items + y;
         it.R = row_of(B, it.b);
@@ -71,14 +73,13 @@ __device__ __forceinline__ Item item_of(const Args &A, int i)
         it.first = i0 / kTile;
         it.per = it.x0 < it.R.len && i1 >= i0 ? i1 / kTile - it.first + 1 : 0;
         const int all = it.per * A.G;
-        it.from = (int)((long long)all * p / parts);
-        it.n = (int)((long long)all * (p + 1) / parts) - it.from;
+        it.from = parts == 1 ? 0 : (int)((long long)all * p / parts);
+        it.n = parts == 1 ? all : (int)((long long)all * (p + 1) / parts) - it.from;
     } else {
         it.keys = false;
-        const int y = i - A.sink_items - A.key_items, heads = A.a.B * A.a.H, x = y % heads;
-        it.b = x / A.a.H;
-        it.h = x % A.a.H;
-        it.x0 = (A.qtiles - 1 - y / heads) * kTile;
+        int x;
+        it.x0 = (A.qtiles - 1 - A.qheads.divmod(i - A.sink_items - A.key_items, x)) * kTile;
+        it.b = A.H.divmod(x, it.h);
         it.part = -1;
         it.R = row_of(B, it.b);
         it.tiles = key_tiles(it.R, it.R.pos + it.x0, it.R.pos + min(it.x0 + kTile, B.nq) - 1);
@@ -91,10 +92,12 @@ struct Y {
 };
 __device__ __forceinline__ Y stream_of(const Args &A, const Item &it, int n)
 {
-    if (!it.keys) return Y{it.b * A.a.Hkv + it.h / A.G, it.tiles.at(n) * kTile};
-    const int u = it.from + n;
-    return Y{it.b * A.a.H + it.h * A.G + u / it.per, (it.first + u % it.per) * kTile};
+    if (!it.keys) return Y{it.b * A.a.Hkv + A.group.div(it.h), it.tiles.at(n) * kTile};
+    const int u = it.from + n, g = A.G == 1 ? 0 : u / it.per;
+    return Y{it.b * A.a.H + it.h * A.G + g, (it.first + u - g * it.per) * kTile};
 }
+// four numbers of shared memory; stays where it stands, so that they do not all come at once
+__device__ __forceinline__ void lds2(uint32_t at, f2 &a, f2 &b) { asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(at)); }
 // The Y tiles of all items of this block, one after the other; items without any are left out.
 struct Walk {
     Item it;
@@ -124,15 +127,6 @@ struct Walk {
     }
 };
 
-// D (128 x DP) += W Y: the weights' columns 0 .. 63 at w, 64 .. 127 at w + 64 (each in what its warps had read)
-template <int DP> __device__ __forceinline__ void product_halves(uint32_t d, uint32_t w, uint32_t y, bool accumulate)
-{
-    constexpr uint32_t idesc = make_idesc_bf16(128, DP, 0, 1);
-    const uint64_t dy = make_smem_desc(y, kTile * 128, 1024);
-#pragma unroll
-    for (int ks = 0; ks < kTile / 16; ++ks) umma_bf16_ts(d, w + (ks >> 2) * 64 + (ks & 3) * 8, dy + ks * 128, idesc, accumulate || ks != 0);
-}
-
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_constant__ Args A)
 {
@@ -144,13 +138,13 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + P::kAbort);
     const Waits wait{abort_flag, A.a.status != nullptr ? A.a.status : reinterpret_cast<int *>(smem + P::kAbort + 4)};
     if (tid == 0) {
-        for (int s = 0; s < P::kXStages; ++s) { mbar_init(sbase + P::bXFull + 8 * s, 1); mbar_init(sbase + P::bXEmpty + 8 * s, 1); }
-        for (int s = 0; s < P::kYStages; ++s) { mbar_init(sbase + P::bYFull + 8 * s, 1); mbar_init(sbase + P::bYEmpty + 8 * s, 1); }
+        for (int s = 0; s < P::kXStages; ++s) { mbar_init(sbase + P::bXFull + 8 * s, 1); mbar_init(sbase + P::bXEmpty + 8 * s, 2); }
+        for (int s = 0; s < P::kYStages; ++s) { mbar_init(sbase + P::bYFull + 8 * s, 1); mbar_init(sbase + P::bYEmpty + 8 * s, 3); mbar_init(sbase + P::bClear + 8 * s, 1); }
         mbar_init(sbase + P::bS, 1);
         mbar_init(sbase + P::bDP, 1);
-        mbar_init(sbase + P::bW1, 8);
-        mbar_init(sbase + P::bW2, 8);
-        mbar_init(sbase + P::bAcc, 1);
+        mbar_init(sbase + P::bW1, 16);
+        mbar_init(sbase + P::bW2, 16);
+        mbar_init(sbase + P::bAcc, 2);
         abort_flag[0] = abort_flag[1] = 0;
         fence_barrier_init();
     }
@@ -158,7 +152,12 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(smem + P::kTmem);
+    // all columns are this block's, so they begin at 0, which the products' addresses take for granted
+    constexpr uint32_t tmem = 0;
+    if (tid == 0 && *reinterpret_cast<volatile uint32_t *>(smem + P::kTmem) != tmem) {
+        *abort_flag = 1;
+        atomicOr(wait.status, 4 /* LOT_DEV_TIMEOUT */);
+    }
     chain_wait();                                          // the row statistics
 
     if (warp == kLoadWarp) {
@@ -197,61 +196,57 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
             for (uint32_t u = n > P::kYStages ? n - P::kYStages : 0; u < n; ++u)
                 for (int x = 0; x < 4096 && !mbar_try_wait(sbase + P::bYFull + 8 * (u % P::kYStages), (u / P::kYStages) & 1); ++x) {}
         }
-    } else if (warp == kMmaWarp) {
+    } else if (warp == kClearWarp) {
+        // Keys that no query of the batch row sees are multiplied by score gradients of zero: they must be numbers.  This warp passes every stage in
+        // turn and gives it free like the products' warps, so that none of its waits is a whole turn ahead or behind.
+        Walk w;
+        uint32_t n = 0;
+        for (w.begin(A); w.more(A); w.next(A), ++n) {
+            const uint32_t s = n % P::kYStages;
+            if (!wait(sbase + P::bYFull + 8 * s, n / P::kYStages)) break;
+            if (!w.it.keys) {
+                const int j0 = w.it.tiles.at(w.tile) * kTile;
+                if (!all_used(w.it.R, j0)) {
+                    clear_unused<DP>(smem + P::kY + s * P::kYBytes, w.it.R, j0, lane);
+                    if (lane == 0) mbar_arrive(sbase + P::bClear + 8 * s);
+                }
+            }
+            if (lane == 0) mbar_arrive(sbase + P::bYEmpty + 8 * s);
+        }
+    } else if (warp >= kMmaWarp) {
+        const int side = warp - kMmaWarp;                  // 0: S and the products with P; 1: dP and the products with dS
+        const uint32_t leader = elect_one(), tile = tmem + (side ? P::cDP : P::cS), acc = tmem + (side ? P::cK : P::cV), ready = sbase + (side ? P::bW2 : P::bW1);
         Walk w, ahead;
         w.begin(A);
         ahead = w;
-        uint32_t g = 0;
-        bool ok = true;
-        auto operands = [&](uint32_t at) {                 // X and Y of the tile `ahead` stands at, number `at` of this block's
-            if (ahead.tile == 0 && !wait(sbase + P::bXFull + 8 * (ahead.count % P::kXStages), ahead.count / P::kXStages)) return false;
-            const uint32_t s = at % P::kYStages;
-            if (!wait(sbase + P::bYFull + 8 * s, at / P::kYStages)) return false;
-            if (!ahead.it.keys) {                          // keys that no query sees are multiplied by zero: they must be numbers
-                const int j0 = ahead.it.tiles.at(ahead.tile) * kTile;
-                if (!all_used(ahead.it.R, j0)) clear_unused<DP>(smem + P::kY + s * P::kYBytes, ahead.it.R, j0, lane);
-            }
+        uint32_t g = 0, cleared = 0;                       // cleared: for each stage, whether its keys were cleared an odd number of times
+        auto product = [&](uint32_t at) {                  // S or dP of the tile `ahead` stands at, number `at` of this block's
+            const uint32_t x = ahead.count % P::kXStages, y = at % P::kYStages;
+            if (ahead.tile == 0 && !wait(sbase + P::bXFull + 8 * x, ahead.count / P::kXStages)) return false;
+            if (!wait(sbase + P::bYFull + 8 * y, at / P::kYStages)) return false;
+            product_rows<DP>(leader, tile, sbase + P::kX + (2 * x + side) * TB, sbase + P::kY + y * P::kYBytes + side * TB);
+            commit_to(leader, sbase + (side ? P::bDP : P::bS));
+            if (ahead.last()) commit_to(leader, sbase + P::bXEmpty + 8 * x);
             return true;
         };
-        auto product = [&](uint32_t at, int side) {        // S (side 0) or dP (1) of that tile
-            if (elect_one()) {
-                product_rows<DP>(tmem + (side ? P::cDP : P::cS), sbase + P::kX + (2 * (ahead.count % P::kXStages) + side) * TB,
-                                 sbase + P::kY + (at % P::kYStages) * P::kYBytes + side * TB);
-                umma_commit(sbase + (side ? P::bDP : P::bS));
-                if (side && ahead.last()) umma_commit(sbase + P::bXEmpty + 8 * (ahead.count % P::kXStages));
-            }
-            __syncwarp();
-        };
-        if (w.more(A)) {
-            ok = operands(0);
-            if (ok) { product(0, 0); product(0, 1); ahead.next(A); }
-        }
+        bool ok = !w.more(A) || product(0);
+        if (w.more(A)) ahead.next(A);
         for (; ok && w.more(A); w.next(A), ++g) {
-            const bool follow = ahead.more(A);
-            const uint32_t y = sbase + P::kY + (g % P::kYStages) * P::kYBytes;
-            ok = wait(sbase + P::bW1, g);
-            if (!ok) break;
-            tc_fence_after();
-            if (w.it.keys) {
-                if (elect_one()) product_halves<DP>(tmem + P::cV, tmem + P::cS, y + TB, w.tile > 0);
-                __syncwarp();
-            }
-            if (follow) {
-                ok = operands(g + 1);
+            const uint32_t s = g % P::kYStages;
+            if (side && !w.it.keys && !all_used(w.it.R, w.it.tiles.at(w.tile) * kTile)) {
+                ok = wait(sbase + P::bClear + 8 * s, cleared >> s);
                 if (!ok) break;
-                product(g + 1, 0);
+                cleared ^= 1u << s;
             }
-            ok = wait(sbase + P::bW2, g);
+            ok = wait(ready, g);
             if (!ok) break;
             tc_fence_after();
-            if (elect_one()) {
-                product_halves<DP>(tmem + P::cK, tmem + P::cDP, y, w.tile > 0);
-                umma_commit(sbase + P::bYEmpty + 8 * (g % P::kYStages));
-                if (w.last()) umma_commit(sbase + P::bAcc);
-            }
-            __syncwarp();
-            if (follow) {
-                product(g + 1, 1);
+            if (side || w.it.keys) product_weights<DP, 4>(leader, acc, tile, sbase + P::kY + s * P::kYBytes + (side ? 0 : TB), w.tile > 0);
+            commit_to(leader, sbase + P::bYEmpty + 8 * s);
+            if (w.last()) commit_to(leader, sbase + P::bAcc);
+            if (ahead.more(A)) {
+                ok = product(g + 1);
+                if (!ok) break;
                 ahead.next(A);
             }
         }
@@ -259,72 +254,99 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
             for (int x = 0; x < 4096; ++x) (void)mbar_try_wait(sbase + P::bAcc, (w.count & 1) ^ 1);
         }
     } else {
-        const int half = warp >> 2, row = (warp & 3) * 32 + lane;
+        const int part4 = warp >> 2, row = (warp & 3) * 32 + lane, col0 = 32 * part4;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const float c = A.a.scale * kLog2e;
+        const f2 c2 = pack2(c, c);
         uint32_t g = 0, count = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < A.items; i += gridDim.x) {
-            const Item it = item_of(A, i);
-            const Row &R = it.R;
+            // What the loop needs of the item, and no more: registers.  This row sees the rows lo .. hi and 0 .. sk of Y; Y's tiles go up by one from yt,
+            // and at wrap_at back (or on) to wrap_to.
+            int left, lo, hi, sk, yt, wrap_at, wrap_to;
+            bool keys;
             float lse2 = kNever, dl = 0.f;
-            if (!it.keys && it.n > 0) {
-                const float *st = A.stat + ((size_t)(it.b * A.a.H + it.h) * A.qtiles + it.x0 / kTile) * (2 * kTile) + row;
-                lse2 = chain_ld(st);
-                dl = chain_ld(st + kTile);
+            {
+                const Item it = item_of(A, i);
+                const Row &R = it.R;
+                keys = it.keys;
+                left = it.n;
+                if (keys) {
+                    const int j = it.x0 + row;
+                    lo = j - R.right - R.pos;
+                    hi = j >= R.len ? -1 : j < R.sinks ? kFar : j + R.left - R.pos;
+                    sk = -1;
+                    wrap_to = it.first;
+                    wrap_at = it.first + it.per;
+                    yt = it.first + (it.n > 0 ? it.from % it.per : 0);
+                } else {
+                    const int p = R.pos + it.x0 + row;
+                    lo = p - R.left;
+                    hi = R.hi(p);
+                    sk = min(hi, R.sinks - 1);
+                    wrap_to = it.tiles.first;
+                    wrap_at = it.tiles.sink;
+                    yt = it.tiles.at(0);
+                    if (it.n > 0) {
+                        const float *st = A.stat + ((size_t)(it.b * A.a.H + it.h) * A.qtiles + it.x0 / kTile) * (2 * kTile) + row;
+                        lse2 = chain_ld(st);
+                        dl = chain_ld(st + kTile);
+                    }
+                }
             }
-            for (int n = 0; ok && n < it.n; ++n, ++g) {
-                const Y y = stream_of(A, it, n);
+            const bool some = left > 0;
+            const f2 l2 = pack2(lse2, lse2), d2 = pack2(dl, dl);
+            for (; ok && left > 0; --left, ++g) {
+                const int y0 = yt * kTile + col0;
+                if (++yt == wrap_at) yt = wrap_to;
                 const uint32_t s = g % P::kYStages;
-                const float *st = reinterpret_cast<const float *>(smem + P::kS + s * P::kStat) + 64 * half;
-                float p[2][32];
+                const uint32_t st = sbase + P::kS + s * P::kStat + 4 * col0;
+                float p[32];
                 ok = wait(sbase + P::bS, g);
                 if (!ok) break;
                 tc_fence_after();
-                tmem_ld32(lanes + P::cS + 64 * half, p[0]);
-                tmem_ld32(lanes + P::cS + 64 * half + 32, p[1]);
-                uint32_t seen[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int y0 = y.row + 64 * half + 32 * k;
-                    seen[k] = it.keys ? seeing(R, R.pos + y0, it.x0 + row) : seen_keys(R, R.pos + it.x0 + row, y0);
-                }
-                if (it.keys) {
+                tmem_ld32(lanes + P::cS + col0, p);
+                const uint32_t seen = bits_between(lo - y0, hi - y0) | bits_between(-y0, sk - y0);
+                const bool part = __any_sync(0xffffffffu, seen != 0xffffffffu);
+                if (keys) {
                     ok = wait(sbase + P::bYFull + 8 * s, g / P::kYStages);      // the columns' statistics
                     if (!ok) break;
                 }
-                settle(p[0]);
-                settle(p[1]);
-                tc_fence_before();
-                __syncwarp();
-                if (!it.keys && lane == 0) mbar_arrive(sbase + P::bW1);
+                settle(p);
+                if (!keys) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(sbase + P::bW1);
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    if (it.keys) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4) {
-                            const float4 x = *reinterpret_cast<const float4 *>(st + 32 * k + e);
-                            p[k][e] = ex2(fmaf(p[k][e], c, -x.x));
-                            p[k][e + 1] = ex2(fmaf(p[k][e + 1], c, -x.y));
-                            p[k][e + 2] = ex2(fmaf(p[k][e + 2], c, -x.z));
-                            p[k][e + 3] = ex2(fmaf(p[k][e + 3], c, -x.w));
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) p[k][e] = ex2(fmaf(p[k][e], c, -lse2));
+                    for (int e = 0; e < 32; e += 2) {
+                        float u, v;
+                        unpack2(fma2(pack2(p[e], p[e + 1]), c2, l2), u, v);
+                        p[e] = ex2(u);
+                        p[e + 1] = ex2(v);
                     }
-                    if (__any_sync(0xffffffffu, seen[k] != 0xffffffffu)) {
+                } else {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) p[k][e] = (seen[k] >> e) & 1u ? p[k][e] : 0.f;
-                    }
-                    if (it.keys) {
-                        uint32_t x[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = tile::pack_bf16(p[k][2 * e], p[k][2 * e + 1]);
-                        tmem_st16(lanes + P::cS + 64 * half + 16 * k, x);
+                    for (int e = 0; e < 32; e += 4) {
+                        f2 x, y;
+                        float u, v;
+                        lds2(st + 4 * e, x, y);
+                        unpack2(fma2(pack2(p[e], p[e + 1]), c2, x), u, v);
+                        p[e] = ex2(u);
+                        p[e + 1] = ex2(v);
+                        unpack2(fma2(pack2(p[e + 2], p[e + 3]), c2, y), u, v);
+                        p[e + 2] = ex2(u);
+                        p[e + 3] = ex2(v);
                     }
                 }
-                if (it.keys) {
+                if (part) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) p[e] = (seen >> e) & 1u ? p[e] : 0.f;
+                }
+                if (keys) {
+                    uint32_t x[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[e] = tile::pack_bf16(p[2 * e], p[2 * e + 1]);
+                    tmem_st16(lanes + P::cS + col0, x);
                     tmem_wait_st();
                     tc_fence_before();
                     __syncwarp();
@@ -333,62 +355,63 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
                 ok = wait(sbase + P::bDP, g);
                 if (!ok) break;
                 tc_fence_after();
+                float dp[32];
+                tmem_ld32(lanes + P::cDP + col0, dp);
+                settle(dp);
+                uint32_t x[16];
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    float dp[32];
-                    uint32_t x[16];
-                    tmem_ld32(lanes + P::cDP + 64 * half + 32 * k, dp);
-                    settle(dp);
-                    if (it.keys) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4) {
-                            const float4 z = *reinterpret_cast<const float4 *>(st + kTile + 32 * k + e);
-                            p[k][e] *= dp[e] - z.x;
-                            p[k][e + 1] *= dp[e + 1] - z.y;
-                            p[k][e + 2] *= dp[e + 2] - z.z;
-                            p[k][e + 3] *= dp[e + 3] - z.w;
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) p[k][e] *= dp[e] - dl;
-                    }
-                    if (__any_sync(0xffffffffu, seen[k] != 0xffffffffu)) {      // not a product with what may be no number
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) p[k][e] = (seen[k] >> e) & 1u ? p[k][e] : 0.f;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) x[e] = tile::pack_bf16(p[k][2 * e], p[k][2 * e + 1]);
-                    tmem_st16(lanes + P::cDP + 64 * half + 16 * k, x);
+                for (int e = 0; e < 32; e += 4) {
+                    f2 u = d2, v = d2;
+                    if (keys) lds2(st + 4 * (kTile + e), u, v);
+                    u = mul2(pack2(p[e], p[e + 1]), add2(pack2(dp[e], dp[e + 1]), u));
+                    v = mul2(pack2(p[e + 2], p[e + 3]), add2(pack2(dp[e + 2], dp[e + 3]), v));
+                    unpack2(u, dp[e], dp[e + 1]);
+                    unpack2(v, dp[e + 2], dp[e + 3]);
                 }
+                if (part) {                                // not a product with what may be no number
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) dp[e] = (seen >> e) & 1u ? dp[e] : 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = tile::pack_bf16(dp[2 * e], dp[2 * e + 1]);
+                tmem_st16(lanes + P::cDP + col0, x);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(sbase + P::bW2);
             }
-            if (ok && it.n > 0) {
+            if (ok && some) {
                 ok = wait(sbase + P::bAcc, count++);
                 tc_fence_after();
             }
-            // keys: the first four warps have dv, the others dk; queries: half of dq's channels each
-            const float nan = __int_as_float(0x7fc00000), f = !ok ? nan : it.keys && half == 0 ? 1.f : A.a.scale;
-            const int r = it.x0 + row, d = A.a.d, rows = it.keys ? A.a.band.nk : A.a.band.nq;
-            const size_t at = (size_t)(it.b * (it.keys ? A.a.Hkv : A.a.H) + it.h) * rows + r;
-            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(it.keys ? (half ? A.a.dk : A.a.dv) : A.a.dq) + at * d;
-            float *part = A.part + ((size_t)max(it.part, 0) * 2 + half) * (kTile * DP) + (size_t)row * DP;
-            const int from = it.keys ? 0 : half * (DP / 2), to = it.keys ? DP : from + DP / 2, acc = it.keys && half == 0 ? P::cV : P::cK;
-            for (int col = from; col < to; col += 32) {
-                float x[32];
-                if (it.n > 0) {
-                    tmem_ld32(lanes + acc + col, x);
-                    settle(x);
+            // keys: eight warps have dv, the others dk, half of the channels each; queries: a quarter (DP = 64: two warps half) of dq's channels each
+            int again = i;
+            asm volatile("" : "+r"(again));                // not kept over the loop
+            const Item it = item_of(A, again);
+            const int which = part4 >> 1;
+            const float nan = __int_as_float(0x7fc00000), f = !ok ? nan : keys && which == 0 ? 1.f : A.a.scale;
+            const int r = it.x0 + row, d = A.a.d, rows = keys ? A.a.band.nk : A.a.band.nq;
+            const size_t at = (size_t)(it.b * (keys ? A.a.Hkv : A.a.H) + it.h) * rows + r;
+            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(keys ? (which ? A.a.dk : A.a.dv) : A.a.dq) + at * d;
+            float *part = A.part + ((size_t)max(it.part, 0) * 2 + which) * (kTile * DP) + (size_t)row * DP;
+            const int span = keys ? DP / 2 : DP >= 128 ? DP / 4 : DP / 2, from = keys ? (part4 & 1) * span : part4 * span, acc = keys && which == 0 ? P::cV : P::cK;
+#pragma unroll 1
+            for (int col = from; col < from + span && col < DP; col += 16) {
+                float x[16];
+                if (some) {
+                    tmem_ld16(lanes + acc + col, x);
+                    tmem_wait_ld();
                 }
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = it.n > 0 || !ok ? x[e] * f : 0.f;
+                for (int e = 0; e < 16; ++e) {
+                    if (some) asm volatile("" : "+f"(x[e]));          // behind the wait
+                    x[e] = some || !ok ? x[e] * f : 0.f;
+                }
                 if (it.part >= 0) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4 *>(part + col + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                    for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(part + col + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
                 } else if (r < rows) {
-                    store_row32(out, col, d, x);
+                    store_row(out, col, d, x);
                 }
             }
         }
@@ -400,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
     if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
 }
 
-// lse2 and D of every row, in tiles of 128 (rows beyond the last: weights of zero).  LANES threads a row, eight channels each.
+// -lse2 and -D of every row, in tiles of 128 (rows beyond the last: weights of zero).  LANES threads a row, eight channels each.
 template <int LANES>
 __global__ void __launch_bounds__(256) stat_kernel(const __nv_bfloat16 *out, const __nv_bfloat16 *dout, const float *lse, float *stat, int nq, int tiles, int d)
 {
@@ -426,8 +449,8 @@ __global__ void __launch_bounds__(256) stat_kernel(const __nv_bfloat16 *out, con
     if (threadIdx.x % LANES == 0) {
         float *o = stat + ((size_t)head * tiles + r / kTile) * (2 * kTile) + r % kTile;
         const bool none = l == neg_inf();
-        o[0] = none ? kNever : l * kLog2e;
-        o[kTile] = none ? 0.f : s;
+        o[0] = none ? kNever : -l * kLog2e;
+        o[kTile] = none ? 0.f : -s;
     }
     chain_wait();
 }
@@ -523,6 +546,13 @@ cudaError_t launch_bwd_tc(const Bwd &a, cudaStream_t st)
     Args A;
     A.a = a;
     A.G = a.H / a.Hkv;
+    A.kheads = fast_div(a.B * a.Hkv);
+    A.qheads = fast_div(a.B * a.H);
+    A.Hkv = fast_div(a.Hkv);
+    A.H = fast_div(a.H);
+    A.group = fast_div(A.G);
+    A.sink_cut = fast_div(c.sink_parts);
+    A.key_cut = fast_div(c.key_parts);
     A.qtiles = c.qtiles;
     A.ktiles = c.ktiles;
     A.sink_tiles = c.sink_tiles;
