@@ -145,6 +145,18 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+// Behind it the columns just requested may be used.
+__device__ __forceinline__ void settle(float (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]),
+                   "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15])::"memory");
+}
 // Behind it the 32 columns just requested may be used.
 __device__ __forceinline__ void settle(float (&v)[32])
 {
@@ -187,10 +199,37 @@ inline FastDiv fast_div(int d)
 }
 
 // ---- barriers -------------------------------------------------------------------------------------------------------------
+// A try suspends the warp for up to kNap nanoseconds: without the hint the waiting warps' loops took half of all issue slots.
+constexpr uint32_t kNap = 100000;
+__device__ __forceinline__ bool try_nap(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity), "r"(kNap) : "memory");
+    return ok != 0;
+}
 struct Waits {                             // bounded waits of one block: the first that gives up ends them all
     volatile int *abort_flag;
     int *status;
-    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t phase) const { return mbar_wait(bar, phase & 1u, abort_flag, status); }
+    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t phase) const
+    {
+        if (try_nap(bar, phase & 1u)) return true;
+        return slow(bar, phase & 1u, abort_flag, status);
+    }
+    static __device__ __noinline__ bool slow(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status)
+    {
+        const uint64_t t0 = global_timer_ns();
+        for (;;) {
+            if (try_nap(bar, parity)) return true;
+            if (*abort_flag) return false;
+            if (global_timer_ns() - t0 > kWaitLimitNs) break;
+        }
+        *abort_flag = 1;
+        atomicOr(status, 4 /* LOT_DEV_TIMEOUT */);
+        return false;
+    }
 };
 
 // host: bf16 tensor [outer][rows][cols], box 64 columns x 128 rows; columns and rows beyond the tensor read as zeros
