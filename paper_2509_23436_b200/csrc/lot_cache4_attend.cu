@@ -514,33 +514,10 @@ __global__ void __launch_bounds__(D) join_kernel(const __grid_constant__ Args A)
     if (ch == 0 && a.lse != nullptr) a.lse[row] = nothing ? neg_inf() : top * kLn2 + logf(sum);
 }
 
-// How a sequence's chunks are split.  The lengths are on the device, so a split is a number of chunks, counted for the longest sequence there may be; a
-// shorter one leaves its last splits nothing to do.  A round is a chunk for each of a block's four warps.  Few sequences: up to eight splits of
-// up to eight rounds, the blocks of a cluster.  Else so many that the blocks fill the SMs four times over, which evens out sequences of different
-// lengths, but none of less than four rounds (a block's beginning and end cost as much as two).
-struct Split {
-    int splits, each, clustered;
-};
-Split split_of(int sms, int B, int Hkv, int tiles, int nk, int nq, int left, int sinks)
+Split attend_split(int B, int H, int Hkv, int nq, int nk, int left, int sinks)
 {
-    // chunks that left + nq tokens in a row may touch, and those of the sinks; never more than there are
-    const long long all = ((long long)nk + kChunk - 1) / kChunk, touched = ((long long)(left < nk ? left : nk) + nq + 2 * (kChunk - 1)) / kChunk + (sinks + kChunk - 1) / kChunk;
-    const long long chunks = touched < all ? touched : all;
-    const long long blocks = (long long)B * Hkv * tiles, rounds = (chunks + kWarps - 1) / kWarps;
-    Split s{1, (int)rounds * kWarps, 0};
-    if (rounds <= 1) return s;
-    const long long at_once = (long long)kBlocks * sms;
-    if (blocks * 2 <= at_once) {                            // a cluster may have eight blocks; a longer sequence takes more than that pays
-        const long long room = at_once / blocks, n = rounds < room ? rounds : room, m = n < 8 ? n : 8, per = (rounds + m - 1) / m;
-        if (per <= 8) return Split{(int)((rounds + per - 1) / per), (int)per * kWarps, 1};
-    }
-    const long long n = (4 * at_once + blocks - 1) / blocks;
-    long long per = (rounds + n - 1) / n;
-    if (per < 4) per = 4;
-    if ((rounds + per - 1) / per > 512) per = (rounds + 511) / 512;
-    s.splits = (int)((rounds + per - 1) / per);
-    s.each = (int)per * kWarps;
-    return s;
+    const int tiles = (H / Hkv * nq + kRows - 1) / kRows;
+    return split_of(device_sm_count(), (long long)B * Hkv * tiles, nk, (long long)(left < nk ? left : nk) + nq, sinks, kChunk, kWarps, kBlocks);
 }
 
 template <int D, typename T> cudaError_t run(const Args &A, cudaStream_t st)
@@ -570,10 +547,10 @@ template <int D, typename T> cudaError_t run(const Args &A, cudaStream_t st)
 size_t attend4_workspace(int dtype, int B, int H, int Hkv, int nq, int d, int nk, int left, int sinks)
 {
     (void)dtype;
-    const int tiles = (H / Hkv * nq + kRows - 1) / kRows;
-    const Split s = split_of(device_sm_count(), B, Hkv, tiles, nk, nq, left, sinks);
+    const size_t tiles = (H / Hkv * nq + kRows - 1) / kRows;
+    const Split s = attend_split(B, H, Hkv, nq, nk, left, sinks);
     if (s.splits == 1 || s.clustered) return 0;
-    return ((size_t)tiles * B * Hkv * s.splits * kRows * (d + 2) * 4 + 255) & ~(size_t)255;
+    return (tiles * B * Hkv * s.splits * kRows * (d + 2) * 4 + 255) & ~(size_t)255;
 }
 
 cudaError_t launch_attend4(const Attend4 &a, cudaStream_t st)
@@ -582,7 +559,7 @@ cudaError_t launch_attend4(const Attend4 &a, cudaStream_t st)
     A.a = a;
     A.G = a.H / a.cache.Hkv;
     A.row_tiles = (A.G * a.band.nq + kRows - 1) / kRows;
-    const Split s = split_of(device_sm_count(), a.B, a.cache.Hkv, A.row_tiles, a.band.nk, a.band.nq, a.band.left, a.band.sinks);
+    const Split s = attend_split(a.B, a.H, a.cache.Hkv, a.band.nq, a.band.nk, a.band.left, a.band.sinks);
     A.splits = s.splits;
     A.each = s.each;
     A.clustered = s.clustered;

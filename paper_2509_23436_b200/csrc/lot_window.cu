@@ -369,7 +369,7 @@ template <typename T, int DP> cudaError_t bwd_t(const Bwd &a, cudaStream_t st)
 cudaError_t launch_fwd(const Fwd &a, cudaStream_t st)
 {
     if (a.dtype == 0) return a.d <= 32 ? fwd_t<float, 32>(a, st) : a.d <= 64 ? fwd_t<float, 64>(a, st) : fwd_t<float, 128>(a, st);
-    return launch_fwd_tc(a, st);
+    return few_supported(a.dtype, a.H, a.Hkv, a.band.nq, a.band.nk) ? launch_few(a, st) : launch_fwd_tc(a, st);
 }
 cudaError_t launch_bwd(const Bwd &a, cudaStream_t st)
 {

@@ -42,9 +42,8 @@ extern "C" {
 
 size_t lot_window_fwd_workspace_bytes(int dtype, int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks)
 {
-    (void)left; (void)right;
-    if (check_sizes(dtype, B, H, Hkv, nq, nk, d, sinks) != LOT_OK) return 0;
-    return 0;
+    if (check_sizes(dtype, B, H, Hkv, nq, nk, d, sinks) != LOT_OK || B == 0 || nq == 0) return 0;
+    return few_supported(dtype, H, Hkv, nq, nk) ? few_workspace(B, H, Hkv, band_of(nullptr, nullptr, nq, nk, left, right, sinks), d) : 0;
 }
 
 int lot_window_fwd(const void *q, const void *k, const void *v, const int32_t *key_len, const int32_t *q_start,
@@ -61,7 +60,7 @@ int lot_window_fwd(const void *q, const void *k, const void *v, const int32_t *k
         return LOT_ERR_INVALID_ARG;
     const size_t need = lot_window_fwd_workspace_bytes(dtype, B, H, Hkv, nq, nk, d, left, right, sinks);
     if (need > 0 && (!ws || !aligned(ws, 256) || ws_bytes < need)) return LOT_ERR_WORKSPACE;
-    const Fwd a{band_of(key_len, q_start, nq, nk, left, right, sinks), q, k, v, out, lse, dtype, B, H, Hkv, d, scale, status};
+    const Fwd a{band_of(key_len, q_start, nq, nk, left, right, sinks), q, k, v, out, lse, dtype, B, H, Hkv, d, scale, status, ws};
     return done(launch_fwd(a, (cudaStream_t)stream));
 }
 

@@ -437,7 +437,7 @@ template <int DP> cudaError_t launch_t(const Args &A, cudaStream_t st)
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                   const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-bool make_tile_map(CUtensorMap *m, const void *base, long long outer, int rows, int cols)
+bool make_tile_map(CUtensorMap *m, const void *base, long long outer, int rows, int cols, int box_rows)
 {
     static EncodeTiledFn fn = [] {
         void *p = nullptr;
@@ -447,7 +447,7 @@ bool make_tile_map(CUtensorMap *m, const void *base, long long outer, int rows, 
     }();
     if (fn == nullptr) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)outer}, strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)rows * cols * 2};
-    const cuuint32_t box[3] = {64u, (cuuint32_t)kTile, 1u}, es[3] = {1u, 1u, 1u};
+    const cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, 1u}, es[3] = {1u, 1u, 1u};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

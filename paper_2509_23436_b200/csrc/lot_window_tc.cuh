@@ -71,7 +71,10 @@ template <int DP> __device__ __forceinline__ void clear_unused(uint8_t *tile, co
     fence_proxy_async_smem();
     __syncwarp();
 }
-__device__ __forceinline__ bool all_used(const Row &R, int j0) { return R.used(j0) && j0 + kTile <= R.len && (j0 >= R.first || j0 + kTile <= R.sinks); }
+template <int ROWS = kTile> __device__ __forceinline__ bool all_used(const Row &R, int j0)
+{
+    return R.used(j0) && j0 + ROWS <= R.len && (j0 >= R.first || j0 + ROWS <= R.sinks);
+}
 
 // ---- products ---------------------------------------------------------------------------------------------------------------
 // The whole warp computes the descriptors, so that they stay in uniform registers; the lane with `leader` set issues (one fixed lane: a branch around
@@ -232,8 +235,8 @@ struct Waits {                             // bounded waits of one block: the fi
     }
 };
 
-// host: bf16 tensor [outer][rows][cols], box 64 columns x 128 rows; columns and rows beyond the tensor read as zeros
-bool make_tile_map(CUtensorMap *m, const void *base, long long outer, int rows, int cols);
+// host: bf16 tensor [outer][rows][cols], box 64 columns x `box` rows; columns and rows beyond the tensor read as zeros
+bool make_tile_map(CUtensorMap *m, const void *base, long long outer, int rows, int cols, int box = kTile);
 
 } // namespace window
 } // namespace lot
