@@ -10,6 +10,7 @@
 #include <mutex>
 
 namespace lot {
+int device_sm_count();
 namespace window {
 namespace {
 
@@ -258,13 +259,49 @@ __global__ void __launch_bounds__(kThreads) dq_kernel(const __grid_constant__ Bw
     }
 }
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ Bwd a)
+size_t delta_bytes(int B, int H, int nq) { return ((size_t)B * H * nq * 4 + 255) & ~(size_t)255; }
+
+// How key tiles are cut: a tile's list (the query tiles of all its query heads that see it) in parts of at most `most` tiles, whose sums merge_kernel adds
+// in order.  Parts of the tiles with sinks (every later query sees them) first, then the others'.
+struct Cut {
+    int tiles, sink_tiles, sink_parts, key_parts;
+    __host__ __device__ int works(int sinks) const { return sinks ? sink_tiles * sink_parts : (tiles - sink_tiles) * key_parts; }
+    __host__ __device__ int all() const { return works(1) + works(0); }
+    __host__ __device__ bool whole() const { return (sink_tiles == 0 || sink_parts == 1) && (tiles == sink_tiles || key_parts == 1); }
+};
+Cut cut_of(int B, int H, int Hkv, int nq, int nk, int left, int right, int sinks)
 {
+    Cut c;
+    c.tiles = (nk + kT - 1) / kT;
+    c.sink_tiles = ((sinks < nk ? sinks : nk) + kT - 1) / kT;
+    const long long qtiles = (nq + kT - 1) / kT, span = ((long long)left + right + kT - 1) / kT + 2, G = H / Hkv;
+    const long long sink_len = G * qtiles, key_len = G * (span < qtiles ? span : qtiles), heads = (long long)B * Hkv;
+    // three blocks an SM: no part longer than a third of a block's share, nor of more than four tiles where that leaves enough of them
+    const long long share = heads * (c.sink_tiles * sink_len + (c.tiles - c.sink_tiles) * key_len) / (9ll * device_sm_count()), most = share > 4 ? share : 4;
+    c.sink_parts = (int)((sink_len + most - 1) / most);
+    c.key_parts = (int)((key_len + most - 1) / most);
+    if (c.sink_parts < 1) c.sink_parts = 1;
+    if (c.key_parts < 1) c.key_parts = 1;
+    return c;
+}
+struct BwdCut {
+    Bwd a;
+    Cut cut;
+    float *part;                           // [B Hkv][part][dk, dv][64][DP], or nullptr: every tile whole
+};
+size_t part_floats(const Cut &c, int B, int Hkv, int DP) { return c.whole() ? 0 : (size_t)B * Hkv * c.all() * 2 * kT * DP; }
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ BwdCut c)
+{
+    const Bwd &a = c.a;
     extern __shared__ __align__(16) float sm[];
     constexpr int LD = Dim<DP>::LD, NC = Dim<DP>::NC;
     float *sQ = sm, *sO = sQ + kT * LD, *sK = sO + kT * LD, *sV = sK + kT * LD, *sP = sV + kT * LD, *sW = sP + kT * (kT + 4), *sL = sW + kT * (kT + 4);
-    const int b = blockIdx.z, hk = blockIdx.y, j0 = blockIdx.x * kT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4, G = a.H / a.Hkv;
+    const int b = blockIdx.z, hk = blockIdx.y, tx = threadIdx.x & 15, ty = threadIdx.x >> 4, G = a.H / a.Hkv;
+    const bool has_sinks = (int)blockIdx.x < c.cut.works(1);
+    const int work = blockIdx.x - (has_sinks ? 0 : c.cut.works(1)), parts = has_sinks ? c.cut.sink_parts : c.cut.key_parts, part = work % parts;
+    const int j0 = (work / parts + (has_sinks ? 0 : c.cut.sink_tiles)) * kT;
     const int nq = a.band.nq, nk = a.band.nk, d = a.d;
     const Row R = row_of(a.band, b);
     const size_t krow = ((size_t)b * a.Hkv + hk) * nk;
@@ -273,41 +310,51 @@ __global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ B
     stage<DP>(sV, static_cast<const T *>(a.v) + krow * d, j0, nk, d, used);
     // queries that see a key of the tile: positions j0 - right .. j0 + 63 + left, all later ones if the tile holds a sink
     const int i0 = max(j0 - R.right - R.pos, 0), i1 = j0 < R.sinks ? nq - 1 : (int)min((long long)nq - 1, (long long)j0 + kT - 1 + R.left - R.pos);
-    const float c = a.scale * kLog2e;
+    const float sc = a.scale * kLog2e;
     float dk[4][NC], dv[4][NC];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int u = 0; u < NC; ++u) dk[i][u] = dv[i][u] = 0.f;
-    if (j0 < R.len) {
-        for (int g = 0; g < G; ++g) {
-            const size_t qrow = ((size_t)b * a.H + hk * G + g) * nq;
-            for (int q0 = i0 / kT * kT; q0 <= i1; q0 += kT) {
-                __syncthreads();
-                stage<DP>(sQ, static_cast<const T *>(a.q) + qrow * d, q0, nq, d, All{});
-                stage<DP>(sO, static_cast<const T *>(a.dout) + qrow * d, q0, nq, d, All{});
-                if (threadIdx.x < kT) {
-                    const int row = min(q0 + (int)threadIdx.x, nq - 1);
-                    sL[threadIdx.x] = a.lse[qrow + row] * kLog2e;
-                    sL[kT + threadIdx.x] = a.delta[qrow + row];
-                }
-                __syncthreads();
-                float s[4][4], dp[4][4];
-                scores<DP>(sK, sQ, ty, tx, s);
-                scores<DP>(sV, sO, ty, tx, dp);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int row = tx + 16 * j, at = (4 * ty + i) * (kT + 4) + row;
-                        const bool seen = q0 + row < nq && R.sees(R.pos + q0 + row, j0 + 4 * ty + i);
-                        weights(seen, s[i][j], dp[i][j], c, a.scale, sL[row], sL[kT + row], sP[at], sW[at]);
-                    }
-                __syncwarp();
-                apply<DP>(sP, sO, ty, tx, dv);
-                apply<DP>(sW, sQ, ty, tx, dk);
-            }
+    const int first = i0 / kT, per = j0 < R.len && i1 >= i0 ? i1 / kT - first + 1 : 0;
+    const int from = (int)((long long)per * G * part / parts), to = (int)((long long)per * G * (part + 1) / parts);
+    for (int u = from; u < to; ++u) {
+        const size_t qrow = ((size_t)b * a.H + hk * G + u / per) * nq;
+        const int q0 = (first + u % per) * kT;
+        __syncthreads();
+        stage<DP>(sQ, static_cast<const T *>(a.q) + qrow * d, q0, nq, d, All{});
+        stage<DP>(sO, static_cast<const T *>(a.dout) + qrow * d, q0, nq, d, All{});
+        if (threadIdx.x < kT) {
+            const int row = min(q0 + (int)threadIdx.x, nq - 1);
+            sL[threadIdx.x] = a.lse[qrow + row] * kLog2e;
+            sL[kT + threadIdx.x] = a.delta[qrow + row];
         }
+        __syncthreads();
+        float s[4][4], dp[4][4];
+        scores<DP>(sK, sQ, ty, tx, s);
+        scores<DP>(sV, sO, ty, tx, dp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = tx + 16 * j, at = (4 * ty + i) * (kT + 4) + row;
+                const bool seen = q0 + row < nq && R.sees(R.pos + q0 + row, j0 + 4 * ty + i);
+                weights(seen, s[i][j], dp[i][j], sc, a.scale, sL[row], sL[kT + row], sP[at], sW[at]);
+            }
+        __syncwarp();
+        apply<DP>(sP, sO, ty, tx, dv);
+        apply<DP>(sW, sQ, ty, tx, dk);
+    }
+    if (c.part != nullptr) {
+        float *o = c.part + (((size_t)b * a.Hkv + hk) * c.cut.all() + blockIdx.x) * (2 * kT * DP);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int u = 0; u < NC; ++u) {
+                o[(4 * ty + i) * DP + channel<DP>(tx, u)] = dk[i][u];
+                o[(kT + 4 * ty + i) * DP + channel<DP>(tx, u)] = dv[i][u];
+            }
+        return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -320,6 +367,28 @@ __global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ B
                 Elem<T>::store(ok + channel<DP>(tx, u), dk[i][u]);
                 Elem<T>::store(ov + channel<DP>(tx, u), dv[i][u]);
             }
+    }
+}
+
+// dk (side 0) and dv of a key tile from its parts, in order
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) merge_kernel(const __grid_constant__ BwdCut c)
+{
+    const Bwd &a = c.a;
+    const int tile = blockIdx.x >> 1, side = blockIdx.x & 1, hk = blockIdx.y, b = blockIdx.z, d = a.d;
+    const bool has_sinks = tile < c.cut.sink_tiles;
+    const int parts = has_sinks ? c.cut.sink_parts : c.cut.key_parts, first = has_sinks ? tile * parts : c.cut.works(1) + (tile - c.cut.sink_tiles) * parts;
+    const float *p = c.part + (((size_t)b * a.Hkv + hk) * c.cut.all() + first) * (2 * kT * DP) + side * (kT * DP);
+    T *out = static_cast<T *>(side ? a.dv : a.dk) + ((size_t)b * a.Hkv + hk) * a.band.nk * d;
+    for (int idx = threadIdx.x; idx < kT * (DP / 4); idx += kThreads) {
+        const int r = idx / (DP / 4), ch = idx % (DP / 4) * 4, row = tile * kT + r;
+        if (row >= a.band.nk || ch >= d) continue;
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < parts; ++k) {
+            const float4 x = *reinterpret_cast<const float4 *>(p + (size_t)k * (2 * kT * DP) + r * DP + ch);
+            o[0] += x.x; o[1] += x.y; o[2] += x.z; o[3] += x.w;
+        }
+        store4(out + (size_t)row * d + ch, o);
     }
 }
 
@@ -361,7 +430,11 @@ template <typename T, int DP> cudaError_t bwd_t(const Bwd &a, cudaStream_t st)
         if (e != cudaSuccess) return e;
     }
     if (a.band.nk == 0) return cudaSuccess;
-    return launch<dkv_kernel<T, DP>>(a, dim3((a.band.nk + kT - 1) / kT, a.Hkv, a.B), (4 * kT * Dim<DP>::LD + 2 * kT * (kT + 4) + 2 * kT) * 4, st);
+    BwdCut c{a, cut_of(a.B, a.H, a.Hkv, a.band.nq, a.band.nk, a.band.left, a.band.right, a.band.sinks), nullptr};
+    if (!c.cut.whole()) c.part = reinterpret_cast<float *>(reinterpret_cast<char *>(a.delta) + delta_bytes(a.B, a.H, a.band.nq));
+    cudaError_t e = launch<dkv_kernel<T, DP>>(c, dim3(c.cut.all(), a.Hkv, a.B), (4 * kT * Dim<DP>::LD + 2 * kT * (kT + 4) + 2 * kT) * 4, st);
+    if (e != cudaSuccess || c.part == nullptr) return e;
+    return launch<merge_kernel<T, DP>>(c, dim3(2 * c.cut.tiles, a.Hkv, a.B), 0, st);
 }
 
 } // namespace
@@ -371,6 +444,12 @@ cudaError_t launch_fwd(const Fwd &a, cudaStream_t st)
     if (a.dtype == 0) return a.d <= 32 ? fwd_t<float, 32>(a, st) : a.d <= 64 ? fwd_t<float, 64>(a, st) : fwd_t<float, 128>(a, st);
     return few_supported(a.dtype, a.H, a.Hkv, a.band.nq, a.band.nk) ? launch_few(a, st) : launch_fwd_tc(a, st);
 }
+size_t bwd_f32_workspace(int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks)
+{
+    const Cut c = cut_of(B, H, Hkv, nq, nk, left, right, sinks);
+    return delta_bytes(B, H, nq) + ((part_floats(c, B, Hkv, d <= 32 ? 32 : d <= 64 ? 64 : 128) * 4 + 255) & ~(size_t)255);
+}
+
 cudaError_t launch_bwd(const Bwd &a, cudaStream_t st)
 {
     if (a.dtype == 0) return a.d <= 32 ? bwd_t<float, 32>(a, st) : a.d <= 64 ? bwd_t<float, 64>(a, st) : bwd_t<float, 128>(a, st);

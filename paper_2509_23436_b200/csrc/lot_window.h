@@ -60,6 +60,7 @@ struct Attend4 {
 cudaError_t launch_fwd(const Fwd &a, cudaStream_t st);
 cudaError_t launch_fwd_tc(const Fwd &a, cudaStream_t st);      // bf16 tensors (lot_window_tc.cu)
 cudaError_t launch_bwd(const Bwd &a, cudaStream_t st);
+size_t bwd_f32_workspace(int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks);
 cudaError_t launch_bwd_tc(const Bwd &a, cudaStream_t st);      // bf16 tensors (lot_window_tc_bwd.cu)
 size_t bwd_tc_workspace(int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks);
 size_t attend4_workspace(int dtype, int B, int H, int Hkv, int nq, int d, int nk, int left, int sinks);

@@ -8,7 +8,6 @@ namespace {
 
 using namespace lot::window;
 
-inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline bool aligned(const void *p, unsigned by) { return (reinterpret_cast<uintptr_t>(p) & (by - 1)) == 0; }
 
 int check_sizes(int dtype, int B, int H, int Hkv, int nq, int nk, int d, int sinks)
@@ -67,9 +66,8 @@ int lot_window_fwd(const void *q, const void *k, const void *v, const int32_t *k
 size_t lot_window_bwd_workspace_bytes(int dtype, int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks)
 {
     if (check_sizes(dtype, B, H, Hkv, nq, nk, d, sinks) != LOT_OK || B == 0) return 0;
-    if (dtype == LOT_F32) return up256((size_t)B * H * nq * 4);
     const Band b = band_of(nullptr, nullptr, nq, nk, left, right, sinks);
-    return bwd_tc_workspace(B, H, Hkv, nq, nk, d, b.left, b.right, b.sinks);
+    return (dtype == LOT_F32 ? bwd_f32_workspace : bwd_tc_workspace)(B, H, Hkv, nq, nk, d, b.left, b.right, b.sinks);
 }
 
 int lot_window_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *dout,
