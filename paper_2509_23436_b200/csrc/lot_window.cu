@@ -1,10 +1,12 @@
-// Window attention with sinks on float32 multiply-adds: forward and backward of float32 tensors.
+// Window attention with sinks of float32 tensors: forward and backward on warp-level tensor-core products.
 //
-// Forward: a block takes 64 queries of a head and goes over the 64-key tiles that any of them sees, first those of the sinks, then the
-// window's, in one pass with the running maximum and sum of the softmax.  Backward: P = exp(S - lse) again, D_i = <dout_i, out_i>,
-// dS = P (dP - D): a block of 64 queries gathers dq over its keys, a block of 64 keys gathers dk and dv over the query heads and the
-// queries that see them, so nothing is added by atomics.
-// A thread holds 4 x 4 scores (rows in sixteen-lane groups) and 4 rows of d / 16 channels of the sums.
+// float32 accuracy from tf32 products: x = hi + lo, hi rounded to tf32's eleven bits, x y = hi hi + hi lo + lo hi up to 2^-22 (three products for one).  On
+// float32 multiply-adds the same kernels ran at a quarter of their rate and took F32_OLD.
+// A block takes 64 rows, a warp 16 of them with all columns, so that the softmax stays inside lane quads and weights become operands of the next
+// product as they lie (a lane's two neighbouring columns are entries t and t + 4 of an operand whose columns are counted accordingly).
+// Forward: 64 queries go over the 64-key tiles that any of them sees, first those of the sinks, then the window's, in one pass with the running
+// maximum and sum.  Backward: P = exp(S - lse) again, D_i = <dout_i, out_i>, dS = P (dP - D): a block of 64 queries gathers dq over its keys, a
+// block of 64 keys gathers dk and dv over the query heads and the queries that see them, so nothing is added by atomics.
 #include "lot_window.cuh"
 
 #include <mutex>
@@ -14,76 +16,99 @@ int device_sm_count();
 namespace window {
 namespace {
 
-constexpr int kT = 64, kThreads = 256;
+constexpr int kT = 64, kThreads = 128;
 
+// rows of a tile in shared memory: 8 numbers of padding, so that four rows' 32-byte pieces, and four rows' 8 neighbours, lie in different banks
 template <int DP> struct Dim {
-    static constexpr int LD = DP + 4, NC = DP / 16;            // padded row of a tile; channels a thread sums
+    static constexpr int LD = DP + 8, NT = DP / 8;             // NT: 8-channel pieces
 };
 
 // 64 rows of x (rows first .. first + 63 below n, channels below d) into s[64][LD]; rows for which keep(row) fails become zeros
-template <int DP, typename T, typename F>
-__device__ __forceinline__ void stage(float *s, const T *x, int first, int n, int d, F keep)
+template <int DP, typename F>
+__device__ __forceinline__ void stage(float *s, const float *x, int first, int n, int d, F keep)
 {
     for (int idx = threadIdx.x; idx < kT * (DP / 4); idx += kThreads) {
         const int r = idx / (DP / 4), c = (idx % (DP / 4)) * 4, row = first + r;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (row < n && c < d && keep(row)) load4(x + (size_t)row * d + c, v);
-        *reinterpret_cast<float4 *>(s + r * Dim<DP>::LD + c) = make_float4(v[0], v[1], v[2], v[3]);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row < n && c < d && keep(row)) v = __ldg(reinterpret_cast<const float4 *>(x + (size_t)row * d + c));
+        *reinterpret_cast<float4 *>(s + r * Dim<DP>::LD + c) = v;
     }
 }
 struct All {
     __device__ __forceinline__ bool operator()(int) const { return true; }
 };
 
-// acc[i][j] = <a row 4 ty + i, b row tx + 16 j>
-template <int DP> __device__ __forceinline__ void scores(const float *a, const float *b, int ty, int tx, float (&acc)[4][4])
+__device__ __forceinline__ void halves(float x, uint32_t &hi, uint32_t &lo)
 {
-    constexpr int LD = Dim<DP>::LD;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < DP; k += 4) {
-        float4 x[4], y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4 *>(a + (4 * ty + i) * LD + k);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4 *>(b + (tx + 16 * j) * LD + k);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                acc[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, acc[i][j]))));
+    hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+    lo = __float_as_uint(x - __uint_as_float(hi));
+}
+__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// d += a b of 16 x 8 and 8 x 8 numbers; a's entries (row g, k t), (row g + 8, k t), (row g, k t + 4), (row g + 8, k t + 4), b's (k t, n g), (k t + 4, n g)
+struct Frag {
+    uint32_t hi[4], lo[4];
+    __device__ __forceinline__ Frag(float a0, float a1, float a2, float a3)
+    {
+        halves(a0, hi[0], lo[0]);
+        halves(a1, hi[1], lo[1]);
+        halves(a2, hi[2], lo[2]);
+        halves(a3, hi[3], lo[3]);
     }
+};
+__device__ __forceinline__ void mma3(float (&d)[4], const Frag &a, float b0, float b1)
+{
+    uint32_t h0, h1, l0, l1;
+    halves(b0, h0, l0);
+    halves(b1, h1, l1);
+    mma_tf32(d, a.lo, h0, h1);
+    mma_tf32(d, a.hi, l0, l1);
+    mma_tf32(d, a.hi, h0, h1);
 }
 
-// channel u of a thread's sums: 4 neighbours of every 64, or DP / 16 neighbours below that
-template <int DP> __device__ __forceinline__ int channel(int tx, int u) { return DP >= 64 ? (u >> 2) * 64 + tx * 4 + (u & 3) : tx * Dim<DP>::NC + u; }
-
-// o[i][u] += sum_k w[4 ty + i][k] x[k][channel u], w with rows of kT + 4
-template <int DP> __device__ __forceinline__ void apply(const float *w, const float *x, int ty, int tx, float (&o)[4][Dim<DP>::NC])
+// acc[n] (16 rows x 8) = <row of a, row 8 n + .. of b> for this warp's rows a[0 .. 15][LD] and 8 N rows of b; channels are taken in pairs
+template <int DP, int N> __device__ __forceinline__ void scores(const float *a, const float *b, float (&acc)[N][4])
 {
-    constexpr int LD = Dim<DP>::LD, NC = Dim<DP>::NC;
+    constexpr int LD = Dim<DP>::LD;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
 #pragma unroll 2
-    for (int k = 0; k < kT; k += 4) {
-        float p[4][4];
+    for (int k = 0; k < DP; k += 8) {
+        const float2 x = *reinterpret_cast<const float2 *>(a + g * LD + k + 2 * t), y = *reinterpret_cast<const float2 *>(a + (g + 8) * LD + k + 2 * t);
+        const Frag f(x.x, y.x, x.y, y.y);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 t = *reinterpret_cast<const float4 *>(w + (4 * ty + i) * (kT + 4) + k);
-            p[i][0] = t.x; p[i][1] = t.y; p[i][2] = t.z; p[i][3] = t.w;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float y[NC];
-#pragma unroll
-            for (int u = 0; u < NC; ++u) y[u] = x[(k + e) * LD + channel<DP>(tx, u)];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int u = 0; u < NC; ++u) o[i][u] = fmaf(p[i][e], y[u], o[i][u]);
+        for (int n = 0; n < N; ++n) {
+            const float2 z = *reinterpret_cast<const float2 *>(b + (8 * n + g) * LD + k + 2 * t);
+            mma3(acc[n], f, z.x, z.y);
         }
     }
+}
+// o[c] (16 rows x 8 channels) += w x, w this warp's 16 x 8 N weights as scores() leaves them, x 8 N rows
+template <int DP, int N> __device__ __forceinline__ void apply(const float (&w)[N][4], const float *x, float (&o)[Dim<DP>::NT][4])
+{
+    constexpr int LD = Dim<DP>::LD;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const Frag f(w[n][0], w[n][2], w[n][1], w[n][3]);      // columns 2 t and 2 t + 1 as entries t and t + 4
+        const float *p = x + (8 * n + 2 * t) * LD + g;
+#pragma unroll
+        for (int c = 0; c < Dim<DP>::NT; ++c) mma3(o[c], f, p[8 * c], p[LD + 8 * c]);
+    }
+}
+// one row of the sums: channels 8 c + 2 t, + 1
+template <int DP> __device__ __forceinline__ void store_sums(float *row, int d, const float (&o)[Dim<DP>::NT][4], int lower, float f)
+{
+    const int t = threadIdx.x & 3;
+#pragma unroll
+    for (int c = 0; c < Dim<DP>::NT; ++c)
+        if (8 * c < d) *reinterpret_cast<float2 *>(row + 8 * c + 2 * t) = make_float2(o[c][2 * lower] * f, o[c][2 * lower + 1] * f);
 }
 
 // Key tiles that queries at positions p0 .. p1 see: those of the sinks below the window's first, then the window's.
@@ -104,82 +129,78 @@ __device__ __forceinline__ Tiles tiles_of(const Row &R, int p0, int p1)
     return t;
 }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ Fwd a)
 {
     extern __shared__ __align__(16) float sm[];
-    constexpr int LD = Dim<DP>::LD, NC = Dim<DP>::NC;
-    float *sQ = sm, *sK = sQ + kT * LD, *sV = sK + kT * LD, *sP = sV + kT * LD;
-    const int b = blockIdx.z, h = blockIdx.y, q0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    constexpr int LD = Dim<DP>::LD, NT = Dim<DP>::NT;
+    float *sQ = sm, *sK = sQ + kT * LD, *sV = sK + kT * LD;
+    const int b = blockIdx.z, h = blockIdx.y, q0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kT, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int nq = a.band.nq, nk = a.band.nk, d = a.d;
     const Row R = row_of(a.band, b);
     const size_t qrow = ((size_t)b * a.H + h) * nq, krow = ((size_t)b * a.Hkv + h / (a.H / a.Hkv)) * nk;
-    const T *k = static_cast<const T *>(a.k) + krow * d, *v = static_cast<const T *>(a.v) + krow * d;
-    stage<DP>(sQ, static_cast<const T *>(a.q) + qrow * d, q0, nq, d, All{});
-    const Tiles t = tiles_of(R, R.pos + q0, R.pos + min(q0 + kT, nq) - 1);
+    const float *k = static_cast<const float *>(a.k) + krow * d, *v = static_cast<const float *>(a.v) + krow * d;
+    stage<DP>(sQ, static_cast<const float *>(a.q) + qrow * d, q0, nq, d, All{});
+    const Tiles tiles = tiles_of(R, R.pos + q0, R.pos + min(q0 + kT, nq) - 1);
     const float c = a.scale * kLog2e;
-    float m[4], l[4], o[4][NC];
+    const int row[2] = {q0 + 16 * warp + g, q0 + 16 * warp + g + 8};
+    float m[2] = {neg_inf(), neg_inf()}, l[2] = {0.f, 0.f}, o[NT][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        m[i] = neg_inf(); l[i] = 0.f;
+    for (int u = 0; u < NT; ++u)
 #pragma unroll
-        for (int u = 0; u < NC; ++u) o[i][u] = 0.f;
-    }
-    for (int it = 0; it < t.count(); ++it) {
-        const int j0 = t.at(it) * kT;
+        for (int e = 0; e < 4; ++e) o[u][e] = 0.f;
+    for (int it = 0; it < tiles.count(); ++it) {
+        const int j0 = tiles.at(it) * kT;
         __syncthreads();
         auto used = [&](int j) { return R.used(j); };
         stage<DP>(sK, k, j0, nk, d, used);
         stage<DP>(sV, v, j0, nk, d, used);
         __syncthreads();
-        float s[4][4];
-        scores<DP>(sQ, sK, ty, tx, s);
+        float s[kT / 8][4];
+        scores<DP, kT / 8>(sQ + 16 * warp * LD, sK, s);
+        // does the whole warp see the whole tile
+        const int pa = R.pos + q0 + 16 * warp;
+        if (!(j0 + kT - 1 <= R.hi(pa) && j0 >= pa + 15 - R.left)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int p = R.pos + q0 + 4 * ty + i;
+            for (int n = 0; n < kT / 8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (!R.sees(R.pos + row[e >> 1], j0 + 8 * n + 2 * t + (e & 1))) s[n][e] = neg_inf();
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
             float top = neg_inf();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                s[i][j] = R.sees(p, j0 + tx + 16 * j) ? s[i][j] * c : neg_inf();
-                top = fmaxf(top, s[i][j]);
-            }
-#pragma unroll
-            for (int w = 1; w < 16; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-            top = fmaxf(top, m[i]);
-            const float ref = top == neg_inf() ? 0.f : top, old = ex2(m[i] - ref);       // nothing visible so far: 0
-            m[i] = top;
+            for (int n = 0; n < kT / 8; ++n) top = fmaxf(top, fmaxf(s[n][2 * r], s[n][2 * r + 1]));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(m[r], c * fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)));
+            const float ref = top == neg_inf() ? 0.f : top, old = ex2(m[r] - ref);       // nothing visible so far: 0
+            m[r] = top;
             float sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                s[i][j] = ex2(s[i][j] - ref);
-                sum += s[i][j];
-                sP[(4 * ty + i) * (kT + 4) + tx + 16 * j] = s[i][j];
+            for (int n = 0; n < kT / 8; ++n) {
+                s[n][2 * r] = ex2(fmaf(s[n][2 * r], c, -ref));
+                s[n][2 * r + 1] = ex2(fmaf(s[n][2 * r + 1], c, -ref));
+                sum += s[n][2 * r] + s[n][2 * r + 1];
             }
+            l[r] = l[r] * old + sum;
 #pragma unroll
-            for (int w = 1; w < 16; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-            l[i] = l[i] * old + sum;
-#pragma unroll
-            for (int u = 0; u < NC; ++u) o[i][u] *= old;
+            for (int u = 0; u < NT; ++u) { o[u][2 * r] *= old; o[u][2 * r + 1] *= old; }
         }
-        __syncwarp();                      // a row's weights are written and read by one half warp
-        apply<DP>(sP, sV, ty, tx, o);
+        apply<DP, kT / 8>(s, sV, o);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = q0 + 4 * ty + i;
-        if (row >= nq) break;
-        const float inv = l[i] > 0.f ? 1.f / l[i] : 0.f;
-        T *out = static_cast<T *>(a.out) + (qrow + row) * d;
-#pragma unroll
-        for (int u = 0; u < NC; ++u)
-            if (channel<DP>(tx, u) < d) Elem<T>::store(out + channel<DP>(tx, u), o[i][u] * inv);
-        if (a.lse != nullptr && tx == 0) a.lse[qrow + row] = l[i] > 0.f ? m[i] * kLn2 + logf(l[i]) : neg_inf();
+    for (int r = 0; r < 2; ++r) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+        if (row[r] >= nq) continue;
+        store_sums<DP>(static_cast<float *>(a.out) + (qrow + row[r]) * d, d, o, r, l[r] > 0.f ? 1.f / l[r] : 0.f);
+        if (a.lse != nullptr && t == 0) a.lse[qrow + row[r]] = l[r] > 0.f ? m[r] * kLn2 + logf(l[r]) : neg_inf();
     }
 }
 
 // delta = <dout, out> of every row: a warp each
-template <typename T>
-__global__ void __launch_bounds__(256) delta_kernel(const T *out, const T *dout, float *delta, long long rows, int d)
+__global__ void __launch_bounds__(256) delta_kernel(const float *out, const float *dout, float *delta, long long rows, int d)
 {
     const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (row >= rows) return;
@@ -196,67 +217,59 @@ __global__ void __launch_bounds__(256) delta_kernel(const T *out, const T *dout,
     if ((threadIdx.x & 31) == 0) delta[row] = s;
 }
 
-// P and dS of one query and key; both zero where the query does not see the key
-__device__ __forceinline__ void weights(bool seen, float s, float dp, float c, float scale, float lse2, float delta, float &p, float &ds)
-{
-    p = seen ? ex2(fmaf(s, c, -lse2)) : 0.f;
-    ds = seen ? p * (dp - delta) * scale : 0.f;
-}
+constexpr int kN = 4;                      // column pieces of 8 at a time in the backward: registers
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads) dq_kernel(const __grid_constant__ Bwd a)
 {
     extern __shared__ __align__(16) float sm[];
-    constexpr int LD = Dim<DP>::LD, NC = Dim<DP>::NC;
-    float *sQ = sm, *sO = sQ + kT * LD, *sK = sO + kT * LD, *sV = sK + kT * LD, *sW = sV + kT * LD;
-    const int b = blockIdx.z, h = blockIdx.y, q0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    constexpr int LD = Dim<DP>::LD, NT = Dim<DP>::NT;
+    float *sQ = sm, *sO = sQ + kT * LD, *sK = sO + kT * LD, *sV = sK + kT * LD;
+    const int b = blockIdx.z, h = blockIdx.y, q0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kT, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int nq = a.band.nq, nk = a.band.nk, d = a.d;
     const Row R = row_of(a.band, b);
     const size_t qrow = ((size_t)b * a.H + h) * nq, krow = ((size_t)b * a.Hkv + h / (a.H / a.Hkv)) * nk;
-    const T *k = static_cast<const T *>(a.k) + krow * d, *v = static_cast<const T *>(a.v) + krow * d;
-    stage<DP>(sQ, static_cast<const T *>(a.q) + qrow * d, q0, nq, d, All{});
-    stage<DP>(sO, static_cast<const T *>(a.dout) + qrow * d, q0, nq, d, All{});
-    const Tiles t = tiles_of(R, R.pos + q0, R.pos + min(q0 + kT, nq) - 1);
+    const float *k = static_cast<const float *>(a.k) + krow * d, *v = static_cast<const float *>(a.v) + krow * d;
+    stage<DP>(sQ, static_cast<const float *>(a.q) + qrow * d, q0, nq, d, All{});
+    stage<DP>(sO, static_cast<const float *>(a.dout) + qrow * d, q0, nq, d, All{});
+    const Tiles tiles = tiles_of(R, R.pos + q0, R.pos + min(q0 + kT, nq) - 1);
     const float c = a.scale * kLog2e;
-    float lse2[4], dl[4], o[4][NC];
+    const int row[2] = {q0 + 16 * warp + g, q0 + 16 * warp + g + 8};
+    float lse2[2], dl[2], o[NT][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = min(q0 + 4 * ty + i, nq - 1);
-        lse2[i] = a.lse[qrow + row] * kLog2e;
-        dl[i] = a.delta[qrow + row];
-#pragma unroll
-        for (int u = 0; u < NC; ++u) o[i][u] = 0.f;
+    for (int r = 0; r < 2; ++r) {
+        lse2[r] = a.lse[qrow + min(row[r], nq - 1)] * kLog2e;
+        dl[r] = a.delta[qrow + min(row[r], nq - 1)];
     }
-    for (int it = 0; it < t.count(); ++it) {
-        const int j0 = t.at(it) * kT;
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[u][e] = 0.f;
+    for (int it = 0; it < tiles.count(); ++it) {
+        const int j0 = tiles.at(it) * kT;
         __syncthreads();
         auto used = [&](int j) { return R.used(j); };
         stage<DP>(sK, k, j0, nk, d, used);
         stage<DP>(sV, v, j0, nk, d, used);
         __syncthreads();
-        float s[4][4], dp[4][4];
-        scores<DP>(sQ, sK, ty, tx, s);
-        scores<DP>(sO, sV, ty, tx, dp);
+#pragma unroll 1
+        for (int n0 = 0; n0 < kT; n0 += 8 * kN) {
+            float s[kN][4], dp[kN][4];
+            scores<DP, kN>(sQ + 16 * warp * LD, sK + n0 * LD, s);
+            scores<DP, kN>(sO + 16 * warp * LD, sV + n0 * LD, dp);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int n = 0; n < kN; ++n)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float p, ds;
-                weights(R.sees(R.pos + q0 + 4 * ty + i, j0 + tx + 16 * j), s[i][j], dp[i][j], c, a.scale, lse2[i], dl[i], p, ds);
-                sW[(4 * ty + i) * (kT + 4) + tx + 16 * j] = ds;
-            }
-        __syncwarp();
-        apply<DP>(sW, sK, ty, tx, o);
+                for (int e = 0; e < 4; ++e) {
+                    const bool seen = R.sees(R.pos + row[e >> 1], j0 + n0 + 8 * n + 2 * t + (e & 1));
+                    s[n][e] = seen ? ex2(fmaf(s[n][e], c, -lse2[e >> 1])) * (dp[n][e] - dl[e >> 1]) : 0.f;
+                }
+            apply<DP, kN>(s, sK + n0 * LD, o);
+        }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = q0 + 4 * ty + i;
-        if (row >= nq) break;
-        T *out = static_cast<T *>(a.dq) + (qrow + row) * d;
-#pragma unroll
-        for (int u = 0; u < NC; ++u)
-            if (channel<DP>(tx, u) < d) Elem<T>::store(out + channel<DP>(tx, u), o[i][u]);
-    }
+    for (int r = 0; r < 2; ++r)
+        if (row[r] < nq) store_sums<DP>(static_cast<float *>(a.dq) + (qrow + row[r]) * d, d, o, r, a.scale);
 }
 
 size_t delta_bytes(int B, int H, int nq) { return ((size_t)B * H * nq * 4 + 255) & ~(size_t)255; }
@@ -291,14 +304,14 @@ struct BwdCut {
 };
 size_t part_floats(const Cut &c, int B, int Hkv, int DP) { return c.whole() ? 0 : (size_t)B * Hkv * c.all() * 2 * kT * DP; }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ BwdCut c)
 {
-    const Bwd &a = c.a;
     extern __shared__ __align__(16) float sm[];
-    constexpr int LD = Dim<DP>::LD, NC = Dim<DP>::NC;
-    float *sQ = sm, *sO = sQ + kT * LD, *sK = sO + kT * LD, *sV = sK + kT * LD, *sP = sV + kT * LD, *sW = sP + kT * (kT + 4), *sL = sW + kT * (kT + 4);
-    const int b = blockIdx.z, hk = blockIdx.y, tx = threadIdx.x & 15, ty = threadIdx.x >> 4, G = a.H / a.Hkv;
+    constexpr int LD = Dim<DP>::LD, NT = Dim<DP>::NT;
+    const Bwd &a = c.a;
+    float *sQ = sm, *sO = sQ + kT * LD, *sK = sO + kT * LD, *sV = sK + kT * LD, *sL = sV + kT * LD;
+    const int b = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, G = a.H / a.Hkv;
     const bool has_sinks = (int)blockIdx.x < c.cut.works(1);
     const int work = blockIdx.x - (has_sinks ? 0 : c.cut.works(1)), parts = has_sinks ? c.cut.sink_parts : c.cut.key_parts, part = work % parts;
     const int j0 = (work / parts + (has_sinks ? 0 : c.cut.sink_tiles)) * kT;
@@ -306,72 +319,71 @@ __global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ B
     const Row R = row_of(a.band, b);
     const size_t krow = ((size_t)b * a.Hkv + hk) * nk;
     auto used = [&](int j) { return R.used(j); };
-    stage<DP>(sK, static_cast<const T *>(a.k) + krow * d, j0, nk, d, used);
-    stage<DP>(sV, static_cast<const T *>(a.v) + krow * d, j0, nk, d, used);
+    stage<DP>(sK, static_cast<const float *>(a.k) + krow * d, j0, nk, d, used);
+    stage<DP>(sV, static_cast<const float *>(a.v) + krow * d, j0, nk, d, used);
     // queries that see a key of the tile: positions j0 - right .. j0 + 63 + left, all later ones if the tile holds a sink
     const int i0 = max(j0 - R.right - R.pos, 0), i1 = j0 < R.sinks ? nq - 1 : (int)min((long long)nq - 1, (long long)j0 + kT - 1 + R.left - R.pos);
     const float sc = a.scale * kLog2e;
-    float dk[4][NC], dv[4][NC];
+    const int row[2] = {j0 + 16 * warp + g, j0 + 16 * warp + g + 8};
+    float dk[NT][4], dv[NT][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int u = 0; u < NT; ++u)
 #pragma unroll
-        for (int u = 0; u < NC; ++u) dk[i][u] = dv[i][u] = 0.f;
+        for (int e = 0; e < 4; ++e) dk[u][e] = dv[u][e] = 0.f;
     const int first = i0 / kT, per = j0 < R.len && i1 >= i0 ? i1 / kT - first + 1 : 0;
     const int from = (int)((long long)per * G * part / parts), to = (int)((long long)per * G * (part + 1) / parts);
     for (int u = from; u < to; ++u) {
         const size_t qrow = ((size_t)b * a.H + hk * G + u / per) * nq;
         const int q0 = (first + u % per) * kT;
         __syncthreads();
-        stage<DP>(sQ, static_cast<const T *>(a.q) + qrow * d, q0, nq, d, All{});
-        stage<DP>(sO, static_cast<const T *>(a.dout) + qrow * d, q0, nq, d, All{});
+        stage<DP>(sQ, static_cast<const float *>(a.q) + qrow * d, q0, nq, d, All{});
+        stage<DP>(sO, static_cast<const float *>(a.dout) + qrow * d, q0, nq, d, All{});
         if (threadIdx.x < kT) {
-            const int row = min(q0 + (int)threadIdx.x, nq - 1);
-            sL[threadIdx.x] = a.lse[qrow + row] * kLog2e;
-            sL[kT + threadIdx.x] = a.delta[qrow + row];
+            const int i = min(q0 + (int)threadIdx.x, nq - 1);
+            sL[threadIdx.x] = a.lse[qrow + i] * kLog2e;
+            sL[kT + threadIdx.x] = a.delta[qrow + i];
         }
         __syncthreads();
-        float s[4][4], dp[4][4];
-        scores<DP>(sK, sQ, ty, tx, s);
-        scores<DP>(sV, sO, ty, tx, dp);
+#pragma unroll 1
+        for (int n0 = 0; n0 < kT; n0 += 8 * kN) {
+            float s[kN][4], dp[kN][4];
+            scores<DP, kN>(sK + 16 * warp * LD, sQ + n0 * LD, s);
+            scores<DP, kN>(sV + 16 * warp * LD, sO + n0 * LD, dp);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int n = 0; n < kN; ++n) {
+                const int col = n0 + 8 * n + 2 * t;
+                const float2 ls = *reinterpret_cast<const float2 *>(sL + col), dl = *reinterpret_cast<const float2 *>(sL + kT + col);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int row = tx + 16 * j, at = (4 * ty + i) * (kT + 4) + row;
-                const bool seen = q0 + row < nq && R.sees(R.pos + q0 + row, j0 + 4 * ty + i);
-                weights(seen, s[i][j], dp[i][j], sc, a.scale, sL[row], sL[kT + row], sP[at], sW[at]);
+                for (int e = 0; e < 4; ++e) {
+                    const int i = q0 + col + (e & 1);
+                    const bool seen = i < nq && R.sees(R.pos + i, row[e >> 1]);
+                    s[n][e] = seen ? ex2(fmaf(s[n][e], sc, -(e & 1 ? ls.y : ls.x))) : 0.f;
+                    dp[n][e] = seen ? s[n][e] * (dp[n][e] - (e & 1 ? dl.y : dl.x)) : 0.f;
+                }
             }
-        __syncwarp();
-        apply<DP>(sP, sO, ty, tx, dv);
-        apply<DP>(sW, sQ, ty, tx, dk);
+            apply<DP, kN>(s, sO + n0 * LD, dv);
+            apply<DP, kN>(dp, sQ + n0 * LD, dk);
+        }
     }
     if (c.part != nullptr) {
         float *o = c.part + (((size_t)b * a.Hkv + hk) * c.cut.all() + blockIdx.x) * (2 * kT * DP);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int u = 0; u < NC; ++u) {
-                o[(4 * ty + i) * DP + channel<DP>(tx, u)] = dk[i][u];
-                o[(kT + 4 * ty + i) * DP + channel<DP>(tx, u)] = dv[i][u];
-            }
+        for (int r = 0; r < 2; ++r) {
+            store_sums<DP>(o + (16 * warp + g + 8 * r) * DP, DP, dk, r, a.scale);
+            store_sums<DP>(o + (kT + 16 * warp + g + 8 * r) * DP, DP, dv, r, 1.f);
+        }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = j0 + 4 * ty + i;
-        if (row >= nk) break;
-        T *ok = static_cast<T *>(a.dk) + (krow + row) * d, *ov = static_cast<T *>(a.dv) + (krow + row) * d;
-#pragma unroll
-        for (int u = 0; u < NC; ++u)
-            if (channel<DP>(tx, u) < d) {
-                Elem<T>::store(ok + channel<DP>(tx, u), dk[i][u]);
-                Elem<T>::store(ov + channel<DP>(tx, u), dv[i][u]);
-            }
-    }
+    for (int r = 0; r < 2; ++r)
+        if (row[r] < nk) {
+            store_sums<DP>(static_cast<float *>(a.dk) + (krow + row[r]) * d, d, dk, r, a.scale);
+            store_sums<DP>(static_cast<float *>(a.dv) + (krow + row[r]) * d, d, dv, r, 1.f);
+        }
 }
 
 // dk (side 0) and dv of a key tile from its parts, in order
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads) merge_kernel(const __grid_constant__ BwdCut c)
 {
     const Bwd &a = c.a;
@@ -379,7 +391,7 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(const __grid_constant__
     const bool has_sinks = tile < c.cut.sink_tiles;
     const int parts = has_sinks ? c.cut.sink_parts : c.cut.key_parts, first = has_sinks ? tile * parts : c.cut.works(1) + (tile - c.cut.sink_tiles) * parts;
     const float *p = c.part + (((size_t)b * a.Hkv + hk) * c.cut.all() + first) * (2 * kT * DP) + side * (kT * DP);
-    T *out = static_cast<T *>(side ? a.dv : a.dk) + ((size_t)b * a.Hkv + hk) * a.band.nk * d;
+    float *out = static_cast<float *>(side ? a.dv : a.dk) + ((size_t)b * a.Hkv + hk) * a.band.nk * d;
     for (int idx = threadIdx.x; idx < kT * (DP / 4); idx += kThreads) {
         const int r = idx / (DP / 4), ch = idx % (DP / 4) * 4, row = tile * kT + r;
         if (row >= a.band.nk || ch >= d) continue;
@@ -415,33 +427,32 @@ template <auto KERN, typename A> cudaError_t launch(const A &a, dim3 grid, int b
     return cudaGetLastError();
 }
 
-template <typename T, int DP> cudaError_t fwd_t(const Fwd &a, cudaStream_t st)
+template <int DP> cudaError_t fwd_t(const Fwd &a, cudaStream_t st)
 {
-    return launch<fwd_kernel<T, DP>>(a, dim3((a.band.nq + kT - 1) / kT, a.H, a.B), (3 * kT * Dim<DP>::LD + kT * (kT + 4)) * 4, st);
+    return launch<fwd_kernel<DP>>(a, dim3((a.band.nq + kT - 1) / kT, a.H, a.B), 3 * kT * Dim<DP>::LD * 4, st);
 }
-template <typename T, int DP> cudaError_t bwd_t(const Bwd &a, cudaStream_t st)
+template <int DP> cudaError_t bwd_t(const Bwd &a, cudaStream_t st)
 {
     const long long rows = (long long)a.B * a.H * a.band.nq;
     if (rows > 0) {
-        delta_kernel<T><<<(unsigned)((rows + 7) / 8), 256, 0, st>>>(static_cast<const T *>(a.out), static_cast<const T *>(a.dout), a.delta, rows, a.d);
+        delta_kernel<<<(unsigned)((rows + 7) / 8), 256, 0, st>>>(static_cast<const float *>(a.out), static_cast<const float *>(a.dout), a.delta, rows, a.d);
         cudaError_t e = cudaGetLastError();
-        if (e == cudaSuccess)
-            e = launch<dq_kernel<T, DP>>(a, dim3((a.band.nq + kT - 1) / kT, a.H, a.B), (4 * kT * Dim<DP>::LD + kT * (kT + 4)) * 4, st);
+        if (e == cudaSuccess) e = launch<dq_kernel<DP>>(a, dim3((a.band.nq + kT - 1) / kT, a.H, a.B), 4 * kT * Dim<DP>::LD * 4, st);
         if (e != cudaSuccess) return e;
     }
     if (a.band.nk == 0) return cudaSuccess;
     BwdCut c{a, cut_of(a.B, a.H, a.Hkv, a.band.nq, a.band.nk, a.band.left, a.band.right, a.band.sinks), nullptr};
     if (!c.cut.whole()) c.part = reinterpret_cast<float *>(reinterpret_cast<char *>(a.delta) + delta_bytes(a.B, a.H, a.band.nq));
-    cudaError_t e = launch<dkv_kernel<T, DP>>(c, dim3(c.cut.all(), a.Hkv, a.B), (4 * kT * Dim<DP>::LD + 2 * kT * (kT + 4) + 2 * kT) * 4, st);
+    cudaError_t e = launch<dkv_kernel<DP>>(c, dim3(c.cut.all(), a.Hkv, a.B), (4 * kT * Dim<DP>::LD + 2 * kT) * 4, st);
     if (e != cudaSuccess || c.part == nullptr) return e;
-    return launch<merge_kernel<T, DP>>(c, dim3(2 * c.cut.tiles, a.Hkv, a.B), 0, st);
+    return launch<merge_kernel<DP>>(c, dim3(2 * c.cut.tiles, a.Hkv, a.B), 0, st);
 }
 
 } // namespace
 
 cudaError_t launch_fwd(const Fwd &a, cudaStream_t st)
 {
-    if (a.dtype == 0) return a.d <= 32 ? fwd_t<float, 32>(a, st) : a.d <= 64 ? fwd_t<float, 64>(a, st) : fwd_t<float, 128>(a, st);
+    if (a.dtype == 0) return a.d <= 32 ? fwd_t<32>(a, st) : a.d <= 64 ? fwd_t<64>(a, st) : fwd_t<128>(a, st);
     return few_supported(a.dtype, a.H, a.Hkv, a.band.nq, a.band.nk) ? launch_few(a, st) : launch_fwd_tc(a, st);
 }
 size_t bwd_f32_workspace(int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks)
@@ -452,7 +463,7 @@ size_t bwd_f32_workspace(int B, int H, int Hkv, int nq, int nk, int d, int left,
 
 cudaError_t launch_bwd(const Bwd &a, cudaStream_t st)
 {
-    if (a.dtype == 0) return a.d <= 32 ? bwd_t<float, 32>(a, st) : a.d <= 64 ? bwd_t<float, 64>(a, st) : bwd_t<float, 128>(a, st);
+    if (a.dtype == 0) return a.d <= 32 ? bwd_t<32>(a, st) : a.d <= 64 ? bwd_t<64>(a, st) : bwd_t<128>(a, st);
     return launch_bwd_tc(a, st);
 }
 
