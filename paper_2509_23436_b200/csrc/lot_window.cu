@@ -16,7 +16,7 @@ int device_sm_count();
 namespace window {
 namespace {
 
-constexpr int kT = 64, kThreads = 128;
+constexpr int kT = 64, kThreads = 128, kN = 4, kPart = 8 * kN;       // columns are worked on in parts of kN pieces of 8; a part that none of a warp's rows sees is left out
 
 // rows of a tile in shared memory: 8 numbers of padding, so that four rows' 32-byte pieces, and four rows' 8 neighbours, lie in different banks
 template <int DP> struct Dim {
@@ -59,14 +59,21 @@ struct Frag {
         halves(a3, hi[3], lo[3]);
     }
 };
-__device__ __forceinline__ void mma3(float (&d)[4], const Frag &a, float b0, float b1)
+// d[n] += a b[n] for N independent sums: a term of all of them before the next, for a warp waits for a sum that it adds to again
+template <int N> __device__ __forceinline__ void mma3(float (*d)[4], const Frag &a, const float2 (&b)[N])
 {
-    uint32_t h0, h1, l0, l1;
-    halves(b0, h0, l0);
-    halves(b1, h1, l1);
-    mma_tf32(d, a.lo, h0, h1);
-    mma_tf32(d, a.hi, l0, l1);
-    mma_tf32(d, a.hi, h0, h1);
+    uint32_t h[N][2], l[N][2];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        halves(b[n].x, h[n][0], l[n][0]);
+        halves(b[n].y, h[n][1], l[n][1]);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) mma_tf32(d[n], a.lo, h[n][0], h[n][1]);
+#pragma unroll
+    for (int n = 0; n < N; ++n) mma_tf32(d[n], a.hi, l[n][0], l[n][1]);
+#pragma unroll
+    for (int n = 0; n < N; ++n) mma_tf32(d[n], a.hi, h[n][0], h[n][1]);
 }
 
 // acc[n] (16 rows x 8) = <row of a, row 8 n + .. of b> for this warp's rows a[0 .. 15][LD] and 8 N rows of b; channels are taken in pairs
@@ -81,25 +88,28 @@ template <int DP, int N> __device__ __forceinline__ void scores(const float *a, 
 #pragma unroll 2
     for (int k = 0; k < DP; k += 8) {
         const float2 x = *reinterpret_cast<const float2 *>(a + g * LD + k + 2 * t), y = *reinterpret_cast<const float2 *>(a + (g + 8) * LD + k + 2 * t);
-        const Frag f(x.x, y.x, x.y, y.y);
+        float2 z[N];
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const float2 z = *reinterpret_cast<const float2 *>(b + (8 * n + g) * LD + k + 2 * t);
-            mma3(acc[n], f, z.x, z.y);
-        }
+        for (int n = 0; n < N; ++n) z[n] = *reinterpret_cast<const float2 *>(b + (8 * n + g) * LD + k + 2 * t);
+        mma3<N>(acc, Frag(x.x, y.x, x.y, y.y), z);
     }
 }
 // o[c] (16 rows x 8 channels) += w x, w this warp's 16 x 8 N weights as scores() leaves them, x 8 N rows
 template <int DP, int N> __device__ __forceinline__ void apply(const float (&w)[N][4], const float *x, float (&o)[Dim<DP>::NT][4])
 {
-    constexpr int LD = Dim<DP>::LD;
+    constexpr int LD = Dim<DP>::LD, C = Dim<DP>::NT < 8 ? Dim<DP>::NT : 8;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         const Frag f(w[n][0], w[n][2], w[n][1], w[n][3]);      // columns 2 t and 2 t + 1 as entries t and t + 4
         const float *p = x + (8 * n + 2 * t) * LD + g;
 #pragma unroll
-        for (int c = 0; c < Dim<DP>::NT; ++c) mma3(o[c], f, p[8 * c], p[LD + 8 * c]);
+        for (int c = 0; c < Dim<DP>::NT; c += C) {
+            float2 z[C];
+#pragma unroll
+            for (int u = 0; u < C; ++u) z[u] = make_float2(p[8 * (c + u)], p[LD + 8 * (c + u)]);
+            mma3<C>(o + c, f, z);
+        }
     }
 }
 // one row of the sums: channels 8 c + 2 t, + 1
@@ -129,6 +139,9 @@ __device__ __forceinline__ Tiles tiles_of(const Row &R, int p0, int p1)
     return t;
 }
 
+// do queries at positions pa .. pb see any of the keys j .. j + kPart - 1
+__device__ __forceinline__ bool touches(const Row &R, int pa, int pb, int j) { return j <= R.hi(pb) && (j + kPart - 1 >= pa - R.left || j < R.sinks); }
+
 template <int DP>
 __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ Fwd a)
 {
@@ -156,38 +169,42 @@ __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ F
         stage<DP>(sK, k, j0, nk, d, used);
         stage<DP>(sV, v, j0, nk, d, used);
         __syncthreads();
-        float s[kT / 8][4];
-        scores<DP, kT / 8>(sQ + 16 * warp * LD, sK, s);
-        // does the whole warp see the whole tile
-        const int pa = R.pos + q0 + 16 * warp;
-        if (!(j0 + kT - 1 <= R.hi(pa) && j0 >= pa + 15 - R.left)) {
+        const int pa = R.pos + q0 + 16 * warp, pb = pa + 15;
+#pragma unroll 1
+        for (int n0 = 0; n0 < kT; n0 += kPart) {
+            const int j = j0 + n0;
+            if (!touches(R, pa, pb, j)) continue;
+            float s[kN][4];
+            scores<DP, kN>(sQ + 16 * warp * LD, sK + n0 * LD, s);
+            if (!(j + kPart - 1 <= R.hi(pa) && j >= pb - R.left)) {
 #pragma unroll
-            for (int n = 0; n < kT / 8; ++n)
+                for (int n = 0; n < kN; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (!R.sees(R.pos + row[e >> 1], j0 + 8 * n + 2 * t + (e & 1))) s[n][e] = neg_inf();
-        }
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            float top = neg_inf();
-#pragma unroll
-            for (int n = 0; n < kT / 8; ++n) top = fmaxf(top, fmaxf(s[n][2 * r], s[n][2 * r + 1]));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(m[r], c * fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)));
-            const float ref = top == neg_inf() ? 0.f : top, old = ex2(m[r] - ref);       // nothing visible so far: 0
-            m[r] = top;
-            float sum = 0.f;
-#pragma unroll
-            for (int n = 0; n < kT / 8; ++n) {
-                s[n][2 * r] = ex2(fmaf(s[n][2 * r], c, -ref));
-                s[n][2 * r + 1] = ex2(fmaf(s[n][2 * r + 1], c, -ref));
-                sum += s[n][2 * r] + s[n][2 * r + 1];
+                    for (int e = 0; e < 4; ++e)
+                        if (!R.sees(R.pos + row[e >> 1], j + 8 * n + 2 * t + (e & 1))) s[n][e] = neg_inf();
             }
-            l[r] = l[r] * old + sum;
 #pragma unroll
-            for (int u = 0; u < NT; ++u) { o[u][2 * r] *= old; o[u][2 * r + 1] *= old; }
+            for (int r = 0; r < 2; ++r) {
+                float top = neg_inf();
+#pragma unroll
+                for (int n = 0; n < kN; ++n) top = fmaxf(top, fmaxf(s[n][2 * r], s[n][2 * r + 1]));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(m[r], c * fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)));
+                const float ref = top == neg_inf() ? 0.f : top, old = ex2(m[r] - ref);       // nothing visible so far: 0
+                m[r] = top;
+                float sum = 0.f;
+#pragma unroll
+                for (int n = 0; n < kN; ++n) {
+                    s[n][2 * r] = ex2(fmaf(s[n][2 * r], c, -ref));
+                    s[n][2 * r + 1] = ex2(fmaf(s[n][2 * r + 1], c, -ref));
+                    sum += s[n][2 * r] + s[n][2 * r + 1];
+                }
+                l[r] = l[r] * old + sum;
+#pragma unroll
+                for (int u = 0; u < NT; ++u) { o[u][2 * r] *= old; o[u][2 * r + 1] *= old; }
+            }
+            apply<DP, kN>(s, sV + n0 * LD, o);
         }
-        apply<DP, kT / 8>(s, sV, o);
     }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
@@ -216,8 +233,6 @@ __global__ void __launch_bounds__(256) delta_kernel(const float *out, const floa
     for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
     if ((threadIdx.x & 31) == 0) delta[row] = s;
 }
-
-constexpr int kN = 4;                      // column pieces of 8 at a time in the backward: registers
 
 template <int DP>
 __global__ void __launch_bounds__(kThreads) dq_kernel(const __grid_constant__ Bwd a)
@@ -253,7 +268,8 @@ __global__ void __launch_bounds__(kThreads) dq_kernel(const __grid_constant__ Bw
         stage<DP>(sV, v, j0, nk, d, used);
         __syncthreads();
 #pragma unroll 1
-        for (int n0 = 0; n0 < kT; n0 += 8 * kN) {
+        for (int n0 = 0; n0 < kT; n0 += kPart) {
+            if (!touches(R, R.pos + q0 + 16 * warp, R.pos + q0 + 16 * warp + 15, j0 + n0)) continue;
             float s[kN][4], dp[kN][4];
             scores<DP, kN>(sQ + 16 * warp * LD, sK + n0 * LD, s);
             scores<DP, kN>(sO + 16 * warp * LD, sV + n0 * LD, dp);
@@ -345,7 +361,10 @@ __global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ B
         }
         __syncthreads();
 #pragma unroll 1
-        for (int n0 = 0; n0 < kT; n0 += 8 * kN) {
+        for (int n0 = 0; n0 < kT; n0 += kPart) {
+            // do the queries q0 + n0 .. + kPart - 1 see any of the warp's keys
+            const int pa = R.pos + q0 + n0, ja = j0 + 16 * warp;
+            if (ja > R.hi(pa + kPart - 1) || (ja + 15 < pa - R.left && ja >= R.sinks)) continue;
             float s[kN][4], dp[kN][4];
             scores<DP, kN>(sK + 16 * warp * LD, sQ + n0 * LD, s);
             scores<DP, kN>(sV + 16 * warp * LD, sO + n0 * LD, dp);
