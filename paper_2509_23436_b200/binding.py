@@ -8,6 +8,7 @@ There is no fallback: if the library cannot be loaded the first call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -334,17 +335,23 @@ def _stream_of(stream, index: int) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _work(ws, need_fn, sizes, index):
-    """A workspace of the size the call asks for, when the caller brings none (the size may depend on the device)."""
+@functools.lru_cache(maxsize=4096)
+def _need(name: str, index: int, sizes) -> int:
+    """Workspace bytes of a call's sizes on a device: host arithmetic, asked once."""
+    return _call(getattr(lib(), name), index, sizes)
+
+
+def _work(ws, name, sizes, index):
+    """A workspace of the size the call asks for, when the caller brings none."""
     if ws is not None:
         return ws
-    need = _call(need_fn, index, sizes)
+    need = _need(name, index, sizes)
     return torch.empty(need, device=f"cuda:{index}", dtype=torch.uint8) if need else None
 
 
 def _like(t, shape, dtype, given, name):
     if given is None:
-        return t.new_empty(shape, dtype=dtype)
+        return torch.empty_like(t) if dtype is t.dtype and shape == t.shape else t.new_empty(shape, dtype=dtype)
     if given.shape != shape:
         raise LotError(f"{name} must be {tuple(shape)}")
     return given
@@ -359,7 +366,7 @@ def lot_window_fwd(q, k, v, *, left, right=0, sinks=0, scale=None, key_len=None,
     out = _like(q, q.shape, dt, out, "out")
     if want_lse or lse is not None:
         lse = _like(q, q.shape[:3], torch.float32, lse, "lse")
-    ws = _work(ws, L.lot_window_fwd_workspace_bytes, sizes[:10], dev)
+    ws = _work(ws, "lot_window_fwd_workspace_bytes", sizes[:10], dev)
     st = _call(L.lot_window_fwd, dev, (*ptrs, *sizes, _ptr(out, "out", dt, dev), _ptr(lse, "lse", torch.float32, dev), _ptr(status, "status", i32, dev),
                                        _ptr(ws, "ws", torch.uint8, dev), 0 if ws is None else ws.numel(), _stream_of(stream, dev)))
     _check(st, "lot_window_fwd")
@@ -376,7 +383,7 @@ def lot_window_bwd(q, k, v, out, lse, dout, *, left, right=0, sinks=0, scale=Non
     ptrs = (_ptr(q, "q", dt, dev), _ptr(k, "k", dt, dev), _ptr(v, "v", dt, dev), _ptr(out, "out", dt, dev), _ptr(lse, "lse", torch.float32, dev),
             _ptr(dout, "dout", dt, dev), _ptr(key_len, "key_len", i32, dev), _ptr(q_start, "q_start", i32, dev))
     dq, dk, dv = _like(q, q.shape, dt, dq, "dq"), _like(k, k.shape, dt, dk, "dk"), _like(v, v.shape, dt, dv, "dv")
-    ws = _work(ws, L.lot_window_bwd_workspace_bytes, sizes[:10], dev)
+    ws = _work(ws, "lot_window_bwd_workspace_bytes", sizes[:10], dev)
     st = _call(L.lot_window_bwd, dev, (*ptrs, *sizes, _ptr(dq, "dq", dt, dev), _ptr(dk, "dk", dt, dev), _ptr(dv, "dv", dt, dev),
                                        _ptr(status, "status", i32, dev), _ptr(ws, "ws", torch.uint8, dev), 0 if ws is None else ws.numel(),
                                        _stream_of(stream, dev)))
@@ -432,7 +439,7 @@ def lot_cache4_read(cache, pages, start, m, *, d, dtype=torch.bfloat16, count=No
     page_size, max_pages, num_pages = _cache4(cache, pages, B, d, Hkv, start=start, count=count)
     dev, i32, shape = cache.get_device(), torch.int32, (B, Hkv, m, d)
     k = _like(cache, shape, dtype, k, "k")
-    v = _like(cache, shape, k.dtype, v, "v")
+    v = _like(k, shape, k.dtype, v, "v")
     st = _call(lib().lot_cache4_read, dev, (
         _ptr(cache, "cache", torch.uint8, dev), _ptr(pages, "pages", i32, dev), _ptr(start, "start", i32, dev), _ptr(count, "count", i32, dev),
         _dtype_code(k), B, Hkv, m, d, page_size, max_pages, num_pages, _ptr(k, "k", k.dtype, dev), _ptr(v, "v", k.dtype, dev),
@@ -454,7 +461,7 @@ def lot_cache4_attention(q, cache, pages, length, *, left=-1, sinks=0, scale=Non
     out = _like(q, q.shape, dt, out, "out")
     if want_lse or lse is not None:
         lse = _like(q, q.shape[:3], torch.float32, lse, "lse")
-    ws = _work(ws, L.lot_cache4_attention_workspace_bytes, (code, B, H, Hkv, nq, d, page_size, max_pages, left, sinks), dev)
+    ws = _work(ws, "lot_cache4_attention_workspace_bytes", (code, B, H, Hkv, nq, d, page_size, max_pages, left, sinks), dev)
     st = _call(L.lot_cache4_attention, dev, (
         *ptrs, code, B, H, Hkv, nq, d, page_size, max_pages, num_pages, left, sinks, float(d ** -0.5 if scale is None else scale),
         _ptr(out, "out", dt, dev), _ptr(lse, "lse", torch.float32, dev), _ptr(status, "status", i32, dev), _ptr(ws, "ws", torch.uint8, dev),

@@ -1,13 +1,18 @@
 // Window attention backward of bf16 tensors on tcgen05.
 //
-// P = 2^(c S - lse2), D_i = <dout_i, out_i>, dS = P (dP - D): dq = scale dS K, dk = scale dS^T Q, dv = P^T dO.  Nothing is added by atomics:
-// one persistent launch goes through two kinds of items,
+// P = 2^(c S - lse2), D_i = sum_j P_ij dP_ij = <dout_i, o_i>, dS = P (dP - D): dq = scale dS K, dk = scale dS^T Q, dv = P^T dO.  Nothing is added
+// by atomics: persistent launches go through two kinds of items, first
 //   queries  128 queries of a head gather dq over the key tiles they see: S = Q K^T, dP = dO V^T, dq += dS K
+// then
 //   keys     128 keys of a key head gather dk, dv over its query heads' query tiles that see them: S^T = K Q^T, dP^T = V dO^T,
 //            dv += P^T dO, dk += dS^T Q
-// (seven products of a pair of tiles where one pass with sums shared by atomics or in memory takes five; with a window those sums would be
-// written and read once for every key tile, several times what the two products cost).  Both kinds are the same loop: a standing pair of
-// tiles X1, X2, a stream of pairs Y1, Y2, S = X1 Y1^T, dP = X2 Y2^T, weights as first operand from tensor memory: [+= P Y2], += dS Y1.
+// (eight products of a pair of tiles where one pass with sums shared by atomics or in memory takes five; with a window those sums would be
+// written and read once for every key tile, several times what the other products cost).
+// D~ = <dout, out> of the rounded output is off by up to 2^-8 |dout| |out|, with few visible keys as much as dS itself: the gradients had three times
+// the error of their own rounding.  With any D~, sum_j P (dP - D~) = D - D~ =: e, so the queries' items sum their float32 score gradients, take
+// e P K off (one more product, which e makes small) and leave the exact D to the keys' items.
+// Both kinds are the same loop: a standing pair of
+// tiles X1, X2, a stream of pairs Y1, Y2, S = X1 Y1^T, dP = X2 Y2^T, weights as first operand from tensor memory: += P Y2 (queries: Y1), += dS Y1.
 // Sixteen warps make the weights (a thread: a row, a quarter of the columns), one loads, one clears keys that no query sees, two issue the
 // products.  P takes the columns of S that its own warps have read, dS those of dP, so the products of one and the exponentials of the other
 // run side by side:
@@ -18,7 +23,6 @@
 #include "lot_window_tc.cuh"
 
 #include <mutex>
-#include <type_traits>
 
 namespace lot {
 namespace window {
@@ -32,7 +36,7 @@ template <int DP> struct Plan {
     static constexpr int kX = 0, kY = kXStages * 2 * kTileBytes<DP>, kYBytes = 2 * kTileBytes<DP>, kS = kY + kYStages * kYBytes, kBars = kS + kYStages * kStat;
     static constexpr int bXFull = kBars, bXEmpty = bXFull + 8 * kXStages, bYFull = bXEmpty + 8 * kXStages, bYEmpty = bYFull + 8 * kYStages,
                          bS = bYEmpty + 8 * kYStages, bDP = bS + 8, bW1 = bDP + 8, bW2 = bW1 + 8, bAcc = bW2 + 8, bClear = bAcc + 8, kAbort = bClear + 8 * kYStages, kTmem = kAbort + 8,
-                         kTotal = kTmem + 8;
+                         kSum = kTmem + 8, kTotal = kSum + 4 * kTile * 4;
     static constexpr int cS = 0, cDP = 128, cV = 256, cK = 256 + DP;
 };
 
@@ -44,22 +48,20 @@ struct Args {
     int G, qtiles, ktiles, sink_tiles;     // of a head
     FastDiv kheads, qheads, Hkv, H, group, sink_cut, key_cut;      // heads of all batch rows, of one; query heads of a key head; parts of a tile
     int sink_parts, key_parts;             // parts of a key tile with and without sinks
-    int sink_items, key_items, items;      // sink tiles' parts first, then the other key tiles', then the queries
+    int sink_items, key_items, begin, items;               // sink tiles' parts first, then the other key tiles', then the queries; this launch's: begin .. items - 1
 };
 
 struct Item {
     Row R;
-    bool keys;                             // which kind
     int b, h, x0, part;                    // h: key head, or query head; x0: first row of X; part: of the float32 sums, or -1
     int first, per, from, n;               // Y tiles: keys: number u = from .. from + n - 1 is head u / per, query tile first + u % per
     KeyTiles tiles;                        // queries: the key tiles
 };
-__device__ __forceinline__ Item item_of(const Args &A, int i)
+template <bool KEYS> __device__ __forceinline__ Item item_of(const Args &A, int i)
 {
     Item it;
     const Band &B = A.a.band;
-    if (i < A.sink_items + A.key_items) {
-        it.keys = true;
+    if constexpr (KEYS) {
         const bool sink = i < A.sink_items;
         const int parts = sink ? A.sink_parts : A.key_parts, y = sink ? i : i - A.sink_items;
         int p, z;
@@ -77,7 +79,6 @@ __device__ __forceinline__ Item item_of(const Args &A, int i)
         it.from = parts == 1 ? 0 : (int)((long long)all * p / parts);
         it.n = parts == 1 ? all : (int)((long long)all * (p + 1) / parts) - it.from;
     } else {
-        it.keys = false;
         int x;
         it.x0 = (A.qtiles - 1 - A.qheads.divmod(i - A.sink_items - A.key_items, x)) * kTile;
         it.b = A.H.divmod(x, it.h);
@@ -91,28 +92,28 @@ __device__ __forceinline__ Item item_of(const Args &A, int i)
 struct Y {
     int outer, row;                        // head (of all batch rows') and first row
 };
-__device__ __forceinline__ Y stream_of(const Args &A, const Item &it, int n)
+template <bool KEYS> __device__ __forceinline__ Y stream_of(const Args &A, const Item &it, int n)
 {
-    if (!it.keys) return Y{it.b * A.a.Hkv + A.group.div(it.h), it.tiles.at(n) * kTile};
+    if constexpr (!KEYS) return Y{it.b * A.a.Hkv + A.group.div(it.h), it.tiles.at(n) * kTile};
     const int u = it.from + n, g = A.G == 1 ? 0 : u / it.per;
     return Y{it.b * A.a.H + it.h * A.G + g, (it.first + u - g * it.per) * kTile};
 }
 // four numbers of shared memory; stays where it stands, so that they do not all come at once
 __device__ __forceinline__ void lds2(uint32_t at, f2 &a, f2 &b) { asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(at)); }
 // The Y tiles of all items of this block, one after the other; items without any are left out.
-struct Walk {
+template <bool KEYS> struct Walk {
     Item it;
     int i, tile, count;
     __device__ __forceinline__ void begin(const Args &A)
     {
-        i = blockIdx.x;
+        i = A.begin + blockIdx.x;
         tile = count = 0;
         find(A);
     }
     __device__ __forceinline__ void find(const Args &A)
     {
         for (; i < A.items; i += gridDim.x) {
-            it = item_of(A, i);
+            it = item_of<KEYS>(A, i);
             if (it.n > 0) return;
         }
     }
@@ -128,7 +129,7 @@ struct Walk {
     }
 };
 
-template <int DP>
+template <int DP, bool KEYS>
 __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_constant__ Args A)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -162,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
     chain_wait();                                          // the row statistics
 
     if (warp == kLoadWarp) {
-        Walk w;
+        Walk<KEYS> w;
         uint32_t n = 0;
         for (w.begin(A); w.more(A); w.next(A), ++n) {
             const Item &it = w.it;
@@ -172,20 +173,20 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
                 if (turn > 0 && !wait(sbase + P::bXEmpty + 8 * s, turn - 1)) break;
                 if (elect_one()) {
                     mbar_arrive_expect_tx(bar, 2 * TB);
-                    const int outer = it.b * (it.keys ? A.a.Hkv : A.a.H) + it.h;
-                    load_tile<DP>(dst, it.keys ? &A.k : &A.q, bar, it.x0, outer);
-                    load_tile<DP>(dst + TB, it.keys ? &A.v : &A.dout, bar, it.x0, outer);
+                    const int outer = it.b * (KEYS ? A.a.Hkv : A.a.H) + it.h;
+                    load_tile<DP>(dst, KEYS ? &A.k : &A.q, bar, it.x0, outer);
+                    load_tile<DP>(dst + TB, KEYS ? &A.v : &A.dout, bar, it.x0, outer);
                 }
                 __syncwarp();
             }
             const uint32_t s = n % P::kYStages, turn = n / P::kYStages, bar = sbase + P::bYFull + 8 * s, dst = sbase + P::kY + s * P::kYBytes;
             if (turn > 0 && !wait(sbase + P::bYEmpty + 8 * s, turn - 1)) break;
-            const Y y = stream_of(A, it, w.tile);
+            const Y y = stream_of<KEYS>(A, it, w.tile);
             if (elect_one()) {
-                mbar_arrive_expect_tx(bar, 2 * TB + (it.keys ? P::kStat : 0));
-                load_tile<DP>(dst, it.keys ? &A.q : &A.k, bar, y.row, y.outer);
-                load_tile<DP>(dst + TB, it.keys ? &A.dout : &A.v, bar, y.row, y.outer);
-                if (it.keys) {
+                mbar_arrive_expect_tx(bar, 2 * TB + (KEYS ? P::kStat : 0));
+                load_tile<DP>(dst, KEYS ? &A.q : &A.k, bar, y.row, y.outer);
+                load_tile<DP>(dst + TB, KEYS ? &A.dout : &A.v, bar, y.row, y.outer);
+                if (KEYS) {
                     const float *st = A.stat + ((size_t)y.outer * A.qtiles + y.row / kTile) * (2 * kTile);
                     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                                  ::"r"(sbase + P::kS + s * P::kStat), "l"(st), "r"(P::kStat), "r"(bar) : "memory");
@@ -200,12 +201,12 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
     } else if (warp == kClearWarp) {
         // Keys that no query of the batch row sees are multiplied by score gradients of zero: they must be numbers.  This warp passes every stage in
         // turn and gives it free like the products' warps, so that none of its waits is a whole turn ahead or behind.
-        Walk w;
+        Walk<KEYS> w;
         uint32_t n = 0;
         for (w.begin(A); w.more(A); w.next(A), ++n) {
             const uint32_t s = n % P::kYStages;
             if (!wait(sbase + P::bYFull + 8 * s, n / P::kYStages)) break;
-            if (!w.it.keys) {
+            if (!KEYS) {
                 const int j0 = w.it.tiles.at(w.tile) * kTile;
                 if (!all_used(w.it.R, j0)) {
                     clear_unused<DP>(smem + P::kY + s * P::kYBytes, w.it.R, j0, lane);
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
     } else if (warp >= kMmaWarp) {
         const int side = warp - kMmaWarp;                  // 0: S and the products with P; 1: dP and the products with dS
         const uint32_t leader = elect_one(), tile = tmem + (side ? P::cDP : P::cS), acc = tmem + (side ? P::cK : P::cV), ready = sbase + (side ? P::bW2 : P::bW1);
-        Walk w, ahead;
+        Walk<KEYS> w, ahead;
         w.begin(A);
         ahead = w;
         uint32_t g = 0, cleared = 0;                       // cleared: for each stage, whether its keys were cleared an odd number of times
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
         if (w.more(A)) ahead.next(A);
         for (; ok && w.more(A); w.next(A), ++g) {
             const uint32_t s = g % P::kYStages;
-            if (side && !w.it.keys && !all_used(w.it.R, w.it.tiles.at(w.tile) * kTile)) {
+            if (!KEYS && !all_used(w.it.R, w.it.tiles.at(w.tile) * kTile)) {
                 ok = wait(sbase + P::bClear + 8 * s, cleared >> s);
                 if (!ok) break;
                 cleared ^= 1u << s;
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
             ok = wait(ready, g);
             if (!ok) break;
             tc_fence_after();
-            if (side || w.it.keys) product_weights<DP, 4>(leader, acc, tile, sbase + P::kY + s * P::kYBytes + (side ? 0 : TB), w.tile > 0);
+            product_weights<DP, 4>(leader, acc, tile, sbase + P::kY + s * P::kYBytes + (side || !KEYS ? 0 : TB), w.tile > 0);
             commit_to(leader, sbase + P::bYEmpty + 8 * s);
             if (w.last()) commit_to(leader, sbase + P::bAcc);
             if (ahead.more(A)) {
@@ -261,18 +262,16 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
         const f2 c2 = pack2(c, c);
         uint32_t g = 0, count = 0;
         bool ok = true;
-        for (int i = blockIdx.x; i < A.items; i += gridDim.x) {
+        for (int i = A.begin + blockIdx.x; i < A.items; i += gridDim.x) {
             // What the loop needs of the item, and no more: registers.  This row sees the rows lo .. hi and 0 .. sk of Y; Y's tiles go up by one from yt,
             // and at wrap_at back (or on) to wrap_to.
             int left, lo, hi, sk, yt, wrap_at, wrap_to;
-            bool keys;
             float lse2 = kNever, dl = 0.f;
             {
-                const Item it = item_of(A, i);
+                const Item it = item_of<KEYS>(A, i);
                 const Row &R = it.R;
-                keys = it.keys;
                 left = it.n;
-                if (keys) {
+                if (KEYS) {
                     const int j = it.x0 + row;
                     lo = j - R.right - R.pos;
                     hi = j >= R.len ? -1 : j < R.sinks ? kFar : j + R.left - R.pos;
@@ -297,9 +296,7 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
             }
             const bool some = left > 0;
             const f2 l2 = pack2(lse2, lse2), d2 = pack2(dl, dl);
-            // the two kinds apart: a question in the loop costs a branch at every use
-            auto through = [&](auto kind) {
-                constexpr bool KEYS = decltype(kind)::value;
+            float sum = 0.f;                               // queries: of this row's score gradients
                 for (; ok && left > 0; --left, ++g) {
                     const int y0 = yt * kTile + col0;
                     if (++yt == wrap_at) yt = wrap_to;
@@ -318,9 +315,6 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
                     }
                     settle(p);
                     if constexpr (!KEYS) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(sbase + P::bW1);
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             float u, v;
@@ -346,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
 #pragma unroll
                         for (int e = 0; e < 32; ++e) p[e] = (seen >> e) & 1u ? p[e] : 0.f;
                     }
-                    if constexpr (KEYS) {
+                    {
                         uint32_t x[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) x[e] = tile::pack_bf16(p[2 * e], p[2 * e + 1]);
@@ -382,7 +376,10 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
                             for (int e = 16 * k; e < 16 * k + 16; ++e) p[e] = (seen >> e) & 1u ? p[e] : 0.f;
                         }
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = tile::pack_bf16(p[16 * k + 2 * e], p[16 * k + 2 * e + 1]);
+                        for (int e = 0; e < 8; ++e) {
+                            if (!KEYS) sum += p[16 * k + 2 * e] + p[16 * k + 2 * e + 1];
+                            x[e] = tile::pack_bf16(p[16 * k + 2 * e], p[16 * k + 2 * e + 1]);
+                        }
                         tmem_st8(lanes + P::cDP + col0 + 8 * k, x);
                     }
                     tmem_wait_st();
@@ -390,41 +387,49 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
                     __syncwarp();
                     if (lane == 0) mbar_arrive(sbase + P::bW2);
                 }
-            };
-            if (keys) through(std::true_type{});
-            else through(std::false_type{});
             if (ok && some) {
                 ok = wait(sbase + P::bAcc, count++);
                 tc_fence_after();
             }
-            // keys: eight warps have dv, the others dk, half of the channels each; queries: a quarter (DP = 64: two warps half) of dq's channels each
             int again = i;
             asm volatile("" : "+r"(again));                // not kept over the loop
-            const Item it = item_of(A, again);
-            const int which = part4 >> 1;
-            const float nan = __int_as_float(0x7fc00000), f = !ok ? nan : keys && which == 0 ? 1.f : A.a.scale;
-            const int r = it.x0 + row, d = A.a.d, rows = keys ? A.a.band.nk : A.a.band.nq;
-            const size_t at = (size_t)(it.b * (keys ? A.a.Hkv : A.a.H) + it.h) * rows + r;
-            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(keys ? (which ? A.a.dk : A.a.dv) : A.a.dq) + at * d;
-            float *part = A.part + ((size_t)max(it.part, 0) * 2 + which) * (kTile * DP) + (size_t)row * DP;
-            const int span = keys ? DP / 2 : DP >= 128 ? DP / 4 : DP / 2, from = keys ? (part4 & 1) * span : part4 * span, acc = keys && which == 0 ? P::cV : P::cK;
+            const Item it = item_of<KEYS>(A, again);
+            const int r = it.x0 + row, d = A.a.d, rows = KEYS ? A.a.band.nk : A.a.band.nq;
+            const size_t at = (size_t)(it.b * (KEYS ? A.a.Hkv : A.a.H) + it.h) * rows + r;
+            float e_row = 0.f;
+            if (!KEYS && some) {
+                float *sums = reinterpret_cast<float *>(smem + P::kSum);
+                sums[part4 * kTile + row] = sum;
+                named_bar_sync(1, 512);
+                e_row = (sums[row] + sums[kTile + row]) + (sums[2 * kTile + row] + sums[3 * kTile + row]);
+                if (part4 == 0) const_cast<float *>(A.stat)[((size_t)(it.b * A.a.H + it.h) * A.qtiles + it.x0 / kTile) * (2 * kTile) + kTile + row] = dl - e_row;
+            }
+            // sixteen channels at a time: keys: eight warps dv, the others dk; queries: dq
+            const float nan = __int_as_float(0x7fc00000);
 #pragma unroll 1
-            for (int col = from; col < from + span && col < DP; col += 16) {
+            for (int n = part4; n < (KEYS ? 2 : 1) * (DP / 16); n += 4) {
+                const int which = KEYS ? n / (DP / 16) : 1, col = n % (DP / 16) * 16;              // 0: dv, 1: dk or dq
+                const float f = !ok ? nan : which ? A.a.scale : 1.f;
                 float x[16];
                 if (some) {
-                    tmem_ld16(lanes + acc + col, x);
-                    tmem_wait_ld();
+                    tmem_ld16(lanes + (which ? P::cK : P::cV) + col, x);
+                    settle(x);
+                    if (!KEYS) {
+                        float y[16];
+                        tmem_ld16(lanes + P::cV + col, y);
+                        settle(y);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = fmaf(-e_row, y[e], x[e]);
+                    }
                 }
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    if (some) asm volatile("" : "+f"(x[e]));          // behind the wait
-                    x[e] = some || !ok ? x[e] * f : 0.f;
-                }
+                for (int e = 0; e < 16; ++e) x[e] = some || !ok ? x[e] * f : 0.f;
                 if (it.part >= 0) {
+                    float *part = A.part + ((size_t)it.part * 2 + which) * (kTile * DP) + (size_t)row * DP;
 #pragma unroll
                     for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(part + col + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
                 } else if (r < rows) {
-                    store_row(out, col, d, x);
+                    store_row(static_cast<__nv_bfloat16 *>(KEYS ? (which ? A.a.dk : A.a.dv) : A.a.dq) + at * d, col, d, x);
                 }
             }
         }
@@ -516,7 +521,7 @@ Cut cut_of(int B, int H, int Hkv, int nq, int nk, int left, int right, int sinks
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t stat_bytes(int B, int H, int qtiles) { return up256((size_t)B * H * qtiles * 2 * kTile * 4); }
 
-template <int DP> cudaError_t launch_t(const Args &A, bool merge, cudaStream_t st)
+template <int DP, bool KEYS> cudaError_t launch_kind(Args A, int begin, int end, cudaStream_t st)
 {
     static std::mutex mu;
     static bool set[64] = {};
@@ -525,11 +530,20 @@ template <int DP> cudaError_t launch_t(const Args &A, bool merge, cudaStream_t s
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!set[dev]) {
-            const cudaError_t e = cudaFuncSetAttribute(bwd_tc_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<DP>::kTotal);
+            const cudaError_t e = cudaFuncSetAttribute(bwd_tc_kernel<DP, KEYS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<DP>::kTotal);
             if (e != cudaSuccess) return e;
             set[dev] = true;
         }
     }
+    if (begin == end) return cudaSuccess;
+    A.begin = begin;
+    A.items = end;
+    const int sms = device_sm_count();
+    return chain_launch(bwd_tc_kernel<DP, KEYS>, dim3(end - begin < sms ? end - begin : sms), kThreads, Plan<DP>::kTotal, st, A);
+}
+
+template <int DP> cudaError_t launch_t(const Args &A, bool merge, cudaStream_t st)
+{
     const long long rows = (long long)A.a.B * A.a.H * A.qtiles * kTile;
     cudaError_t e = cudaSuccess;
     if (rows > 0) {
@@ -537,8 +551,9 @@ template <int DP> cudaError_t launch_t(const Args &A, bool merge, cudaStream_t s
                                                                               A.a.lse, const_cast<float *>(A.stat), A.a.band.nq, A.qtiles, A.a.d);
         e = cudaGetLastError();
     }
-    const int sms = device_sm_count();
-    if (e == cudaSuccess) e = chain_launch(bwd_tc_kernel<DP>, dim3(A.items < sms ? A.items : sms), kThreads, Plan<DP>::kTotal, st, A);
+    const int keys = A.sink_items + A.key_items;
+    if (e == cudaSuccess) e = launch_kind<DP, false>(A, keys, A.items, st);
+    if (e == cudaSuccess) e = launch_kind<DP, true>(A, 0, keys, st);
     if (e != cudaSuccess || !merge) return e;
     const int heads = A.a.B * A.a.Hkv;
     const int work = (A.sink_parts > 1 ? A.sink_tiles * heads : 0) + (A.key_parts > 1 ? (A.ktiles - A.sink_tiles) * heads : 0);
