@@ -10,7 +10,8 @@
 // written and read once for every key tile, several times what the other products cost).
 // D~ = <dout, out> of the rounded output is off by up to 2^-8 |dout| |out|, with few visible keys as much as dS itself: the gradients had three times
 // the error of their own rounding.  With any D~, sum_j P (dP - D~) = D - D~ =: e, so the queries' items sum their float32 score gradients, take
-// e P K off (one more product, which e makes small) and leave the exact D to the keys' items.
+// e P K off (one more product, which e makes small) and leave the exact D to the keys' items.  For dq e is the sum of the score gradients as they
+// were rounded for the product: that takes the part of their roundings' error along the keys' mean off too.
 // Both kinds are the same loop: a standing pair of
 // tiles X1, X2, a stream of pairs Y1, Y2, S = X1 Y1^T, dP = X2 Y2^T, weights as first operand from tensor memory: += P Y2 (queries: Y1), += dS Y1.
 // Sixteen warps make the weights (a thread: a row, a quarter of the columns), one loads, one clears keys that no query sees, two issue the
@@ -36,7 +37,7 @@ template <int DP> struct Plan {
     static constexpr int kX = 0, kY = kXStages * 2 * kTileBytes<DP>, kYBytes = 2 * kTileBytes<DP>, kS = kY + kYStages * kYBytes, kBars = kS + kYStages * kStat;
     static constexpr int bXFull = kBars, bXEmpty = bXFull + 8 * kXStages, bYFull = bXEmpty + 8 * kXStages, bYEmpty = bYFull + 8 * kYStages,
                          bS = bYEmpty + 8 * kYStages, bDP = bS + 8, bW1 = bDP + 8, bW2 = bW1 + 8, bAcc = bW2 + 8, bClear = bAcc + 8, kAbort = bClear + 8 * kYStages, kTmem = kAbort + 8,
-                         kSum = kTmem + 8, kTotal = kSum + 4 * kTile * 4;
+                         kSum = kTmem + 8, kTotal = kSum + 8 * kTile * 4;
     static constexpr int cS = 0, cDP = 128, cV = 256, cK = 256 + DP;
 };
 
@@ -296,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
             }
             const bool some = left > 0;
             const f2 l2 = pack2(lse2, lse2), d2 = pack2(dl, dl);
-            float sum = 0.f;                               // queries: of this row's score gradients
+            float sum = 0.f, rounded = 0.f;                // queries: of this row's score gradients, and of what the products take for them
                 for (; ok && left > 0; --left, ++g) {
                     const int y0 = yt * kTile + col0;
                     if (++yt == wrap_at) yt = wrap_to;
@@ -377,8 +378,11 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
                         }
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            if (!KEYS) sum += p[16 * k + 2 * e] + p[16 * k + 2 * e + 1];
                             x[e] = tile::pack_bf16(p[16 * k + 2 * e], p[16 * k + 2 * e + 1]);
+                            if (!KEYS) {
+                                sum += p[16 * k + 2 * e] + p[16 * k + 2 * e + 1];
+                                rounded += __uint_as_float(x[e] << 16) + __uint_as_float(x[e] & 0xffff0000u);
+                            }
                         }
                         tmem_st8(lanes + P::cDP + col0 + 8 * k, x);
                     }
@@ -400,9 +404,13 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
             if (!KEYS && some) {
                 float *sums = reinterpret_cast<float *>(smem + P::kSum);
                 sums[part4 * kTile + row] = sum;
+                sums[(4 + part4) * kTile + row] = rounded;
                 named_bar_sync(1, 512);
+                if (part4 == 0)
+                    const_cast<float *>(A.stat)[((size_t)(it.b * A.a.H + it.h) * A.qtiles + it.x0 / kTile) * (2 * kTile) + kTile + row] =
+                        dl - ((sums[row] + sums[kTile + row]) + (sums[2 * kTile + row] + sums[3 * kTile + row]));
+                sums += 4 * kTile;
                 e_row = (sums[row] + sums[kTile + row]) + (sums[2 * kTile + row] + sums[3 * kTile + row]);
-                if (part4 == 0) const_cast<float *>(A.stat)[((size_t)(it.b * A.a.H + it.h) * A.qtiles + it.x0 / kTile) * (2 * kTile) + kTile + row] = dl - e_row;
             }
             // sixteen channels at a time: keys: eight warps dv, the others dk; queries: dq
             const float nan = __int_as_float(0x7fc00000);
