@@ -1,7 +1,9 @@
 // Window attention with sinks of float32 tensors: forward and backward on warp-level tensor-core products.
 //
 // float32 accuracy from tf32 products: x = hi + lo, hi rounded to tf32's eleven bits, x y = hi hi + hi lo + lo hi up to 2^-22 (three products for one).  On
-// float32 multiply-adds the same kernels ran at a quarter of their rate and took F32_OLD.
+// float32 multiply-adds the same kernels took 62 us where these take 27 (32 sequences of 197 tokens, 3 heads of 64
+// channels, windows of 32 keys on either side), and 311 where they take 116 (forward and backward of 2 x 1001 tokens, 8 heads of 32 channels, 255 keys back).  Three bf16 terms and six products of half the time
+// each took 31 and 133: splitting an operand costs more than its products.
 // A block takes 64 rows, a warp 16 of them with all columns, so that the softmax stays inside lane quads and weights become operands of the next
 // product as they lie (a lane's two neighbouring columns are entries t and t + 4 of an operand whose columns are counted accordingly).
 // Forward: 64 queries go over the 64-key tiles that any of them sees, first those of the sinks, then the window's, in one pass with the running
@@ -23,11 +25,11 @@ template <int DP> struct Dim {
     static constexpr int LD = DP + 8, NT = DP / 8;             // NT: 8-channel pieces
 };
 
-// 64 rows of x (rows first .. first + 63 below n, channels below d) into s[64][LD]; rows for which keep(row) fails become zeros
-template <int DP, typename F>
+// ROWS rows of x (from `first`, below n; channels below d) into s[ROWS][LD]; rows for which keep(row) fails become zeros
+template <int DP, int ROWS = kT, typename F>
 __device__ __forceinline__ void stage(float *s, const float *x, int first, int n, int d, F keep)
 {
-    for (int idx = threadIdx.x; idx < kT * (DP / 4); idx += kThreads) {
+    for (int idx = threadIdx.x; idx < ROWS * (DP / 4); idx += kThreads) {
         const int r = idx / (DP / 4), c = (idx % (DP / 4)) * 4, row = first + r;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (row < n && c < d && keep(row)) v = __ldg(reinterpret_cast<const float4 *>(x + (size_t)row * d + c));
@@ -59,8 +61,10 @@ struct Frag {
         halves(a3, hi[3], lo[3]);
     }
 };
-// d[n] += a b[n] for N independent sums: a term of all of them before the next, for a warp waits for a sum that it adds to again
-template <int N> __device__ __forceinline__ void mma3(float (*d)[4], const Frag &a, const float2 (&b)[N])
+// d[n] += hi hi, e[n] += lo hi + hi lo of a b[n] for N independent sums: a term of all of them before the next, for a warp waits for a sum that it adds
+// to again.  The instruction rounds its sums towards zero, so a sum is kept short, and apart from the small terms: into one long sum the error was 1.2e-6
+// (windows of 65 keys) to 4.9e-6 (of 256, gradients) of the outputs' norm, now it is 3.5e-7 and 5e-7.
+template <int N> __device__ __forceinline__ void mma3(float (*d)[4], float (*e)[4], const Frag &a, const float2 (&b)[N])
 {
     uint32_t h[N][2], l[N][2];
 #pragma unroll
@@ -69,11 +73,18 @@ template <int N> __device__ __forceinline__ void mma3(float (*d)[4], const Frag 
         halves(b[n].y, h[n][1], l[n][1]);
     }
 #pragma unroll
-    for (int n = 0; n < N; ++n) mma_tf32(d[n], a.lo, h[n][0], h[n][1]);
-#pragma unroll
-    for (int n = 0; n < N; ++n) mma_tf32(d[n], a.hi, l[n][0], l[n][1]);
+    for (int n = 0; n < N; ++n) mma_tf32(e[n], a.lo, h[n][0], h[n][1]);
 #pragma unroll
     for (int n = 0; n < N; ++n) mma_tf32(d[n], a.hi, h[n][0], h[n][1]);
+#pragma unroll
+    for (int n = 0; n < N; ++n) mma_tf32(e[n], a.hi, l[n][0], l[n][1]);
+}
+template <int N> __device__ __forceinline__ void clear(float (&x)[N][4])
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[n][e] = 0.f;
 }
 
 // acc[n] (16 rows x 8) = <row of a, row 8 n + .. of b> for this warp's rows a[0 .. 15][LD] and 8 N rows of b; channels are taken in pairs
@@ -81,35 +92,44 @@ template <int DP, int N> __device__ __forceinline__ void scores(const float *a, 
 {
     constexpr int LD = Dim<DP>::LD;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
+    float small[N][4];
+    clear(acc);
+    clear(small);
 #pragma unroll 2
     for (int k = 0; k < DP; k += 8) {
         const float2 x = *reinterpret_cast<const float2 *>(a + g * LD + k + 2 * t), y = *reinterpret_cast<const float2 *>(a + (g + 8) * LD + k + 2 * t);
         float2 z[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) z[n] = *reinterpret_cast<const float2 *>(b + (8 * n + g) * LD + k + 2 * t);
-        mma3<N>(acc, Frag(x.x, y.x, x.y, y.y), z);
+        mma3<N>(acc, small, Frag(x.x, y.x, x.y, y.y), z);
     }
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[n][e] += small[n][e];
 }
 // o[c] (16 rows x 8 channels) += w x, w this warp's 16 x 8 N weights as scores() leaves them, x 8 N rows
 template <int DP, int N> __device__ __forceinline__ void apply(const float (&w)[N][4], const float *x, float (&o)[Dim<DP>::NT][4])
 {
-    constexpr int LD = Dim<DP>::LD, C = Dim<DP>::NT < 8 ? Dim<DP>::NT : 8;
+    constexpr int LD = Dim<DP>::LD, C = 4;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const float *p = x + 2 * t * LD + g;
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const Frag f(w[n][0], w[n][2], w[n][1], w[n][3]);      // columns 2 t and 2 t + 1 as entries t and t + 4
-        const float *p = x + (8 * n + 2 * t) * LD + g;
+    for (int c = 0; c < Dim<DP>::NT; c += C) {
+        float sum[C][4], small[C][4];
+        clear(sum);
+        clear(small);
 #pragma unroll
-        for (int c = 0; c < Dim<DP>::NT; c += C) {
+        for (int n = 0; n < N; ++n) {
             float2 z[C];
 #pragma unroll
-            for (int u = 0; u < C; ++u) z[u] = make_float2(p[8 * (c + u)], p[LD + 8 * (c + u)]);
-            mma3<C>(o + c, f, z);
+            for (int u = 0; u < C; ++u) z[u] = make_float2(p[8 * n * LD + 8 * (c + u)], p[(8 * n + 1) * LD + 8 * (c + u)]);
+            mma3<C>(sum, small, Frag(w[n][0], w[n][2], w[n][1], w[n][3]), z);      // columns 2 t and 2 t + 1 as entries t and t + 4
         }
+#pragma unroll
+        for (int u = 0; u < C; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c + u][e] += sum[u][e] + small[u][e];
     }
 }
 // one row of the sums: channels 8 c + 2 t, + 1
@@ -173,7 +193,7 @@ __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ F
 #pragma unroll 1
         for (int n0 = 0; n0 < kT; n0 += kPart) {
             const int j = j0 + n0;
-            if (!touches(R, pa, pb, j)) continue;
+            if (q0 + 16 * warp >= nq || !touches(R, pa, pb, j)) continue;
             float s[kN][4];
             scores<DP, kN>(sQ + 16 * warp * LD, sK + n0 * LD, s);
             if (!(j + kPart - 1 <= R.hi(pa) && j >= pb - R.left)) {
@@ -214,6 +234,142 @@ __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ F
         store_sums<DP>(static_cast<float *>(a.out) + (qrow + row[r]) * d, d, o, r, l[r] > 0.f ? 1.f / l[r] : 0.f);
         if (a.lse != nullptr && t == 0) a.lse[qrow + row[r]] = l[r] > 0.f ? m[r] * kLn2 + logf(l[r]) : neg_inf();
     }
+}
+
+// ---- few queries: sixteen rows of a key head (its query heads times the queries, which lie in a row) a block, which goes over a part of the key tiles;
+// a warp takes sixteen keys of each.  The warps join in shared memory, the blocks of a row tile in few_join_kernel.  8 x 16 heads on 4, 8192 keys of 128
+// channels, one query: 142 us, 1.9 TB/s (a block waits for its tile, then works on it; two blocks an SM overlap). ----
+constexpr int kFewRows = 16, kFewKeys = kT / (kThreads / 32);
+
+struct Few {
+    Fwd a;
+    int G, splits, each;                   // key tiles of a split
+    float *part;                           // splits > 1: [B Hkv][row tile][split][kFewRows][DP + 2]
+};
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ Few f)
+{
+    extern __shared__ __align__(16) float sm[];
+    constexpr int LD = Dim<DP>::LD, NT = Dim<DP>::NT, N = kFewKeys / 8, OWN = kFewRows * DP + 2 * kFewRows;
+    static_assert(4 * OWN <= 2 * kT * LD, "the warps' sums take the tiles' place");
+    const Fwd &a = f.a;
+    float *sQ = sm, *sK = sQ + kFewRows * LD, *sV = sK + kT * LD;
+    const int split = blockIdx.x % f.splits, r0 = blockIdx.x / f.splits * kFewRows, hk = blockIdx.y, b = blockIdx.z;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, nq = a.band.nq, nk = a.band.nk, d = a.d, rows = f.G * nq;
+    const Row R = row_of(a.band, b);
+    const size_t qrow = ((size_t)b * a.H + (size_t)hk * f.G) * nq, krow = ((size_t)b * a.Hkv + hk) * nk;
+    const float *k = static_cast<const float *>(a.k) + krow * d, *v = static_cast<const float *>(a.v) + krow * d;
+    stage<DP, kFewRows>(sQ, static_cast<const float *>(a.q) + qrow * d, r0, rows, d, All{});
+    const int p0 = R.pos, p1 = R.pos + nq - 1, pos[2] = {p0 + min(r0 + g, rows - 1) % nq, p0 + min(r0 + g + 8, rows - 1) % nq};
+    const Tiles tiles = tiles_of(R, p0, p1);
+    const int to = min(tiles.count(), (split + 1) * f.each);
+    const float c = a.scale * kLog2e;
+    float m[2] = {neg_inf(), neg_inf()}, l[2] = {0.f, 0.f}, o[NT][4];
+    clear(o);
+    for (int it = split * f.each; it < to; ++it) {
+        const int j0 = tiles.at(it) * kT, j = j0 + kFewKeys * warp;
+        __syncthreads();
+        auto used = [&](int i) { return R.used(i); };
+        stage<DP>(sK, k, j0, nk, d, used);
+        stage<DP>(sV, v, j0, nk, d, used);
+        __syncthreads();
+        if (j > R.hi(p1) || (j + kFewKeys - 1 < p0 - R.left && j >= R.sinks)) continue;
+        float s[N][4];
+        scores<DP, N>(sQ, sK + kFewKeys * warp * LD, s);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            float top = neg_inf();
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 2 * r; e < 2 * r + 2; ++e) {
+                    if (!R.sees(pos[r], j + 8 * n + 2 * t + (e & 1))) s[n][e] = neg_inf();
+                    top = fmaxf(top, s[n][e]);
+                }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(m[r], c * fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)));
+            const float ref = top == neg_inf() ? 0.f : top, old = ex2(m[r] - ref);
+            m[r] = top;
+            float sum = 0.f;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 2 * r; e < 2 * r + 2; ++e) {
+                    s[n][e] = ex2(fmaf(s[n][e], c, -ref));
+                    sum += s[n][e];
+                }
+            l[r] = l[r] * old + sum;
+#pragma unroll
+            for (int u = 0; u < NT; ++u) { o[u][2 * r] *= old; o[u][2 * r + 1] *= old; }
+        }
+        apply<DP, N>(s, sV + kFewKeys * warp * LD, o);
+    }
+    __syncthreads();                                       // every warp has left the tiles
+    float *own = sK + warp * OWN;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+        store_sums<DP>(own + (g + 8 * r) * DP, DP, o, r, 1.f);
+        if (t == 0) { own[kFewRows * DP + g + 8 * r] = m[r]; own[kFewRows * DP + kFewRows + g + 8 * r] = l[r]; }
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < kFewRows * DP; idx += kThreads) {
+        const int r = idx / DP, col = idx % DP;
+        if (r0 + r >= rows) break;
+        float top = neg_inf(), sum = 0.f, x = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, sK[w * OWN + kFewRows * DP + r]);
+        const float at = top == neg_inf() ? 0.f : top;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float e = ex2(sK[w * OWN + kFewRows * DP + r] - at);
+            sum += e * sK[w * OWN + kFewRows * DP + kFewRows + r];
+            x += e * sK[w * OWN + idx];
+        }
+        if (f.splits > 1) {
+            float *p = f.part + ((((size_t)b * a.Hkv + hk) * (gridDim.x / f.splits) + blockIdx.x / f.splits) * f.splits + split) * (kFewRows * (DP + 2)) + r * (DP + 2);
+            p[col] = x;
+            if (col == 0) { p[DP] = top; p[DP + 1] = sum; }
+            continue;
+        }
+        if (col < d) static_cast<float *>(a.out)[(qrow + r0 + r) * d + col] = sum > 0.f ? x / sum : 0.f;
+        if (col == 0 && a.lse != nullptr) a.lse[qrow + r0 + r] = sum > 0.f ? top * kLn2 + logf(sum) : neg_inf();
+    }
+}
+// a block joins the splits of one row, a thread a channel
+template <int DP>
+__global__ void __launch_bounds__(DP) few_join_kernel(const __grid_constant__ Few f)
+{
+    const Fwd &a = f.a;
+    const int r = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, col = threadIdx.x, rows = f.G * a.band.nq;
+    constexpr size_t STEP = kFewRows * (DP + 2);
+    const float *p = f.part + (((size_t)b * a.Hkv + hk) * ((rows + kFewRows - 1) / kFewRows) + r / kFewRows) * f.splits * STEP + r % kFewRows * (DP + 2);
+    float top = neg_inf(), sum = 0.f, x = 0.f;
+    for (int i = 0; i < f.splits; ++i) top = fmaxf(top, p[i * STEP + DP]);
+    const float at = top == neg_inf() ? 0.f : top;
+    for (int i = 0; i < f.splits; ++i) {
+        const float e = ex2(p[i * STEP + DP] - at);
+        sum += e * p[i * STEP + DP + 1];
+        x += e * p[i * STEP + col];
+    }
+    const size_t row = ((size_t)b * a.H + (size_t)hk * f.G) * a.band.nq + r;
+    if (col < a.d) static_cast<float *>(a.out)[row * a.d + col] = sum > 0.f ? x / sum : 0.f;
+    if (col == 0 && a.lse != nullptr) a.lse[row] = sum > 0.f ? top * kLn2 + logf(sum) : neg_inf();
+}
+// two waves of blocks, of two tiles at least
+Few few_of(const Fwd &a)
+{
+    Few f{a, a.H / a.Hkv, 1, 1, static_cast<float *>(a.ws)};
+    const Band &n = a.band;
+    const long long tiles = (f.G * n.nq + kFewRows - 1) / kFewRows, blocks = tiles * a.B * a.Hkv, slots = (a.d <= 64 ? 8ll : 4ll) * device_sm_count();
+    const long long run = (long long)(n.left < n.nk ? n.left : n.nk) + (n.right < n.nk ? n.right : n.nk) + n.nq, all = (n.nk + kT - 1) / kT;
+    const long long touched = (run + 2 * (kT - 1)) / kT + (n.sinks + kT - 1) / kT, len = touched < all ? touched : all, parts = slots / blocks > 1 ? slots / blocks : 1;
+    const long long each = (len + parts - 1) / parts;
+    f.each = (int)(each > 2 ? each : 2);
+    f.splits = len > f.each ? (int)((len + f.each - 1) / f.each) : 1;
+    return f;
 }
 
 // delta = <dout, out> of every row: a warp each
@@ -446,8 +602,20 @@ template <auto KERN, typename A> cudaError_t launch(const A &a, dim3 grid, int b
     return cudaGetLastError();
 }
 
+// Few queries: up to 32, and up to 64 of few heads.  A block of fwd_kernel would leave rows empty, not share a key head's keys, and go over all of its keys
+// by itself.  32 heads on 4 key heads of 128 channels, 16384 keys: one query 45 us against 2540, 32 380 against 2610, 64 790 against 2400; 8 x 16 heads on
+// 4, 8192 keys: 33 queries 967 against 1620.
+bool few_f32(int B, int H, int nq) { return nq <= 32 || (nq <= 64 && (long long)B * H * nq <= 32ll * device_sm_count()); }
+
 template <int DP> cudaError_t fwd_t(const Fwd &a, cudaStream_t st)
 {
+    if (few_f32(a.B, a.H, a.band.nq)) {
+        const Few f = few_of(a);
+        const cudaError_t e = launch<few_kernel<DP>>(f, dim3((f.G * a.band.nq + kFewRows - 1) / kFewRows * f.splits, a.Hkv, a.B), (kFewRows + 2 * kT) * Dim<DP>::LD * 4, st);
+        if (e != cudaSuccess || f.splits == 1) return e;
+        few_join_kernel<DP><<<dim3(f.G * a.band.nq, a.Hkv, a.B), DP, 0, st>>>(f);
+        return cudaGetLastError();
+    }
     return launch<fwd_kernel<DP>>(a, dim3((a.band.nq + kT - 1) / kT, a.H, a.B), 3 * kT * Dim<DP>::LD * 4, st);
 }
 template <int DP> cudaError_t bwd_t(const Bwd &a, cudaStream_t st)
@@ -472,7 +640,18 @@ template <int DP> cudaError_t bwd_t(const Bwd &a, cudaStream_t st)
 cudaError_t launch_fwd(const Fwd &a, cudaStream_t st)
 {
     if (a.dtype == 0) return a.d <= 32 ? fwd_t<32>(a, st) : a.d <= 64 ? fwd_t<64>(a, st) : fwd_t<128>(a, st);
-    return few_supported(a.dtype, a.H, a.Hkv, a.band.nq, a.band.nk) ? launch_few(a, st) : launch_fwd_tc(a, st);
+    return few_supported(a.B, a.H, a.Hkv, a.band.nq, a.band.nk) ? launch_few(a, st) : launch_fwd_tc(a, st);
+}
+size_t fwd_workspace(int dtype, int B, int H, int Hkv, const Band &band, int d)
+{
+    if (dtype != 0) return few_supported(B, H, Hkv, band.nq, band.nk) ? few_workspace(B, H, Hkv, band, d) : 0;
+    if (!few_f32(B, H, band.nq)) return 0;
+    Fwd a{};
+    a.band = band;
+    a.B = B; a.H = H; a.Hkv = Hkv; a.d = d;
+    const Few f = few_of(a);
+    const size_t rows = (f.G * band.nq + kFewRows - 1) / kFewRows * kFewRows, DP = d <= 32 ? 32 : d <= 64 ? 64 : 128;
+    return f.splits == 1 ? 0 : ((size_t)B * Hkv * rows * f.splits * (DP + 2) * 4 + 255) & ~(size_t)255;
 }
 size_t bwd_f32_workspace(int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks)
 {

@@ -60,6 +60,7 @@ struct Attend4 {
 cudaError_t launch_fwd(const Fwd &a, cudaStream_t st);
 cudaError_t launch_fwd_tc(const Fwd &a, cudaStream_t st);      // bf16 tensors (lot_window_tc.cu)
 cudaError_t launch_bwd(const Bwd &a, cudaStream_t st);
+size_t fwd_workspace(int dtype, int B, int H, int Hkv, const Band &band, int d);
 size_t bwd_f32_workspace(int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks);
 cudaError_t launch_bwd_tc(const Bwd &a, cudaStream_t st);      // bf16 tensors (lot_window_tc_bwd.cu)
 size_t bwd_tc_workspace(int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks);
@@ -99,7 +100,7 @@ inline Split split_of(int sms, long long blocks, int nk, long long run, int sink
     return s;
 }
 
-bool few_supported(int dtype, int H, int Hkv, int nq, int nk);      // lot_window_few.cu
+bool few_supported(int B, int H, int Hkv, int nq, int nk);         // lot_window_few.cu
 size_t few_workspace(int B, int H, int Hkv, const Band &b, int d);
 cudaError_t launch_few(const Fwd &a, cudaStream_t st);
 

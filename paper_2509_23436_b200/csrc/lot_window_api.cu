@@ -42,7 +42,7 @@ extern "C" {
 size_t lot_window_fwd_workspace_bytes(int dtype, int B, int H, int Hkv, int nq, int nk, int d, int left, int right, int sinks)
 {
     if (check_sizes(dtype, B, H, Hkv, nq, nk, d, sinks) != LOT_OK || B == 0 || nq == 0) return 0;
-    return few_supported(dtype, H, Hkv, nq, nk) ? few_workspace(B, H, Hkv, band_of(nullptr, nullptr, nq, nk, left, right, sinks), d) : 0;
+    return fwd_workspace(dtype, B, H, Hkv, band_of(nullptr, nullptr, nq, nk, left, right, sinks), d);
 }
 
 int lot_window_fwd(const void *q, const void *k, const void *v, const int32_t *key_len, const int32_t *q_start,

@@ -1,5 +1,5 @@
-// What the tcgen05 kernels of window attention share: tiles of 128 rows in shared memory, key tiles a block of queries sees, masks of 32
-// columns, products with the first operand in tensor memory.
+// What the tcgen05 kernels of window attention share: tiles of 128 rows in shared memory, key tiles a block of queries sees, products with the
+// first operand in tensor memory, bounded waits.
 #pragma once
 
 #include "lot_sm100.cuh"
@@ -35,18 +35,6 @@ __device__ __forceinline__ uint32_t bits_between(int a, int b)      // bits a ..
     b = min(b, 31);
     return a > b ? 0u : (0xffffffffu >> (31 - b)) & (0xffffffffu << a);
 }
-// which of the keys j .. j + 31 the query at p sees
-__device__ __forceinline__ uint32_t seen_keys(const Row &R, int p, int j)
-{
-    const int hi = R.hi(p) - j;
-    return bits_between(p - R.left - j, hi) | bits_between(0, min(hi, R.sinks - 1 - j));
-}
-// which of the queries at positions p .. p + 31 see key j
-__device__ __forceinline__ uint32_t seeing(const Row &R, int p, int j)
-{
-    if (j >= R.len) return 0u;
-    return bits_between(j - R.right - p, j < R.sinks ? 31 : j + R.left - p);
-}
 
 // ---- shared memory: a tile is DP / 64 panels of 128 rows x 128 bytes, 16-byte chunks permuted by the row (128-byte swizzle) ----
 template <int DP> constexpr int kTileBytes = kTile * DP * 2;
@@ -77,8 +65,7 @@ template <int ROWS = kTile> __device__ __forceinline__ bool all_used(const Row &
 }
 
 // ---- products ---------------------------------------------------------------------------------------------------------------
-// The whole warp computes the descriptors, so that they stay in uniform registers; the lane with `leader` set issues (one fixed lane: a branch around
-// the products, and addresses in ordinary registers, made the issue of eight products take twice as long as the products).
+// The whole warp computes the descriptors; the lane with `leader` set, always the same one, issues: its products and the commit behind them stay in order.
 // D (tensor memory, 128 x N) = or += A B; descriptors as low word (address) and high word
 __device__ __forceinline__ void issue_ss(uint32_t leader, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate)
 {
@@ -131,16 +118,6 @@ template <int DP, int PARTS> __device__ __forceinline__ void product_weights(uin
 }
 
 // ---- tensor memory ------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r)
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -202,7 +179,7 @@ inline FastDiv fast_div(int d)
 }
 
 // ---- barriers -------------------------------------------------------------------------------------------------------------
-// A try suspends the warp for up to kNap nanoseconds: without the hint the waiting warps' loops took half of all issue slots.
+// A try suspends the warp for up to kNap nanoseconds, so that a waiting warp is not counted among those that could issue.
 constexpr uint32_t kNap = 100000;
 __device__ __forceinline__ bool try_nap(uint32_t bar, uint32_t parity)
 {

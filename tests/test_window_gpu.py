@@ -72,6 +72,16 @@ def test_lengths(nq, nk, left, sinks, dtype):
     both(*draw(nq, 2, 4, 2, nq, nk, 64, dtype), left, 0, sinks)
 
 
+# more query rows of a key head than one tile of any kernel takes, at the last numbers of queries that count as few and the first that do not
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("B,H,Hkv,nq,nk,d,left,right,sinks", [(1, 3, 1, 7, 2100, 32, -1, 0, 0), (2, 8, 2, 17, 1300, 64, 500, 0, 3), (1, 32, 4, 33, 700, 128, 90, 5, 70),
+                                                              (1, 4, 4, 32, 5000, 64, 4000, 0, 1), (1, 6, 2, 64, 900, 96, -1, -1, 0), (1, 2, 1, 65, 900, 64, 200, 0, 2),
+                                                              (40, 5, 5, 31, 130, 40, 20, 0, 1), (1, 1, 1, 1, 20000, 128, -1, 0, 0)])
+def test_few_queries(B, H, Hkv, nq, nk, d, left, right, sinks, dtype):
+    lens = [nk - 11 * b % nk for b in range(B)]
+    both(*draw(nq, B, H, Hkv, nq, nk, d, dtype), left, right, sinks, key_len=lens, q_start=[max(n - nq, -nq // 2) for n in lens], backward=False)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("nq,nk", [(300, 300), (1, 900), (5, 900)])
 def test_padding_and_starts(nq, nk, dtype):
