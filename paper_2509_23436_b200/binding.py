@@ -7,6 +7,7 @@ There is no fallback: if the library cannot be loaded the first call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -341,6 +342,15 @@ def _need(name: str, index: int, sizes) -> int:
     return _call(getattr(lib(), name), index, sizes)
 
 
+def _on(stream, index: int):
+    """Where a call's own tensors are made: on its stream, as if that were current, so that their memory is handed on in its order."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=index) if int(stream) else torch.cuda.default_stream(index)
+    return torch.cuda.stream(stream)
+
+
 def _work(ws, name, sizes, index):
     """A workspace of the size the call asks for, when the caller brings none."""
     if ws is not None:
@@ -363,10 +373,11 @@ def lot_window_fwd(q, k, v, *, left, right=0, sinks=0, scale=None, key_len=None,
     sizes = _band(q, k, v, key_len, q_start, left, right, sinks, scale)
     L, dev, dt, i32 = lib(), q.get_device(), q.dtype, torch.int32
     ptrs = (_ptr(q, "q", dt, dev), _ptr(k, "k", dt, dev), _ptr(v, "v", dt, dev), _ptr(key_len, "key_len", i32, dev), _ptr(q_start, "q_start", i32, dev))
-    out = _like(q, q.shape, dt, out, "out")
-    if want_lse or lse is not None:
-        lse = _like(q, q.shape[:3], torch.float32, lse, "lse")
-    ws = _work(ws, "lot_window_fwd_workspace_bytes", sizes[:10], dev)
+    with _on(stream, dev):
+        out = _like(q, q.shape, dt, out, "out")
+        if want_lse or lse is not None:
+            lse = _like(q, q.shape[:3], torch.float32, lse, "lse")
+        ws = _work(ws, "lot_window_fwd_workspace_bytes", sizes[:10], dev)
     st = _call(L.lot_window_fwd, dev, (*ptrs, *sizes, _ptr(out, "out", dt, dev), _ptr(lse, "lse", torch.float32, dev), _ptr(status, "status", i32, dev),
                                        _ptr(ws, "ws", torch.uint8, dev), 0 if ws is None else ws.numel(), _stream_of(stream, dev)))
     _check(st, "lot_window_fwd")
@@ -382,8 +393,9 @@ def lot_window_bwd(q, k, v, out, lse, dout, *, left, right=0, sinks=0, scale=Non
     L, dev, dt, i32 = lib(), q.get_device(), q.dtype, torch.int32
     ptrs = (_ptr(q, "q", dt, dev), _ptr(k, "k", dt, dev), _ptr(v, "v", dt, dev), _ptr(out, "out", dt, dev), _ptr(lse, "lse", torch.float32, dev),
             _ptr(dout, "dout", dt, dev), _ptr(key_len, "key_len", i32, dev), _ptr(q_start, "q_start", i32, dev))
-    dq, dk, dv = _like(q, q.shape, dt, dq, "dq"), _like(k, k.shape, dt, dk, "dk"), _like(v, v.shape, dt, dv, "dv")
-    ws = _work(ws, "lot_window_bwd_workspace_bytes", sizes[:10], dev)
+    with _on(stream, dev):
+        dq, dk, dv = _like(q, q.shape, dt, dq, "dq"), _like(k, k.shape, dt, dk, "dk"), _like(v, v.shape, dt, dv, "dv")
+        ws = _work(ws, "lot_window_bwd_workspace_bytes", sizes[:10], dev)
     st = _call(L.lot_window_bwd, dev, (*ptrs, *sizes, _ptr(dq, "dq", dt, dev), _ptr(dk, "dk", dt, dev), _ptr(dv, "dv", dt, dev),
                                        _ptr(status, "status", i32, dev), _ptr(ws, "ws", torch.uint8, dev), 0 if ws is None else ws.numel(),
                                        _stream_of(stream, dev)))
@@ -438,8 +450,9 @@ def lot_cache4_read(cache, pages, start, m, *, d, dtype=torch.bfloat16, count=No
     B, Hkv = pages.shape[0], cache.shape[1]
     page_size, max_pages, num_pages = _cache4(cache, pages, B, d, Hkv, start=start, count=count)
     dev, i32, shape = cache.get_device(), torch.int32, (B, Hkv, m, d)
-    k = _like(cache, shape, dtype, k, "k")
-    v = _like(k, shape, k.dtype, v, "v")
+    with _on(stream, dev):
+        k = _like(cache, shape, dtype, k, "k")
+        v = _like(k, shape, k.dtype, v, "v")
     st = _call(lib().lot_cache4_read, dev, (
         _ptr(cache, "cache", torch.uint8, dev), _ptr(pages, "pages", i32, dev), _ptr(start, "start", i32, dev), _ptr(count, "count", i32, dev),
         _dtype_code(k), B, Hkv, m, d, page_size, max_pages, num_pages, _ptr(k, "k", k.dtype, dev), _ptr(v, "v", k.dtype, dev),
@@ -458,10 +471,11 @@ def lot_cache4_attention(q, cache, pages, length, *, left=-1, sinks=0, scale=Non
     page_size, max_pages, num_pages = _cache4(cache, pages, B, d, Hkv, length=length)
     L, dev, dt, i32, code, left, sinks = lib(), q.get_device(), q.dtype, torch.int32, _dtype_code(q), int(left), int(sinks)
     ptrs = (_ptr(q, "q", dt, dev), _ptr(cache, "cache", torch.uint8, dev), _ptr(pages, "pages", i32, dev), _ptr(length, "length", i32, dev))
-    out = _like(q, q.shape, dt, out, "out")
-    if want_lse or lse is not None:
-        lse = _like(q, q.shape[:3], torch.float32, lse, "lse")
-    ws = _work(ws, "lot_cache4_attention_workspace_bytes", (code, B, H, Hkv, nq, d, page_size, max_pages, left, sinks), dev)
+    with _on(stream, dev):
+        out = _like(q, q.shape, dt, out, "out")
+        if want_lse or lse is not None:
+            lse = _like(q, q.shape[:3], torch.float32, lse, "lse")
+        ws = _work(ws, "lot_cache4_attention_workspace_bytes", (code, B, H, Hkv, nq, d, page_size, max_pages, left, sinks), dev)
     st = _call(L.lot_cache4_attention, dev, (
         *ptrs, code, B, H, Hkv, nq, d, page_size, max_pages, num_pages, left, sinks, float(d ** -0.5 if scale is None else scale),
         _ptr(out, "out", dt, dev), _ptr(lse, "lse", torch.float32, dev), _ptr(status, "status", i32, dev), _ptr(ws, "ws", torch.uint8, dev),

@@ -191,6 +191,37 @@ def test_outputs_may_be_given_and_only_they_are_written():
     assert (pool[0] == 7).all() and (pool[2] == 7).all() and not (pool[1] == 7).all()
 
 
+@pytest.mark.parametrize("raw", [False, True])
+def test_a_call_on_another_stream_makes_its_tensors_there(raw):
+    """The current stream still writes memory that it has given back: a call on another stream must not get it for its results."""
+    q, k, v, dout = draw(17, 2, 4, 2, 300, 300, 64, BF)
+    lens, table = torch.full((2,), 300, device=DEV, dtype=torch.int32), torch.arange(10, device=DEV, dtype=torch.int32).view(2, 5)
+    cache = lot.lot_cache4_empty(10, 2, 64, 64, DEV)
+    lot.lot_cache4_write(cache, table, k, v, torch.zeros(2, device=DEV, dtype=torch.int32))
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if raw else side
+
+    def calls(s):
+        out, lse, ws = lot.lot_window_fwd(q, k, v, left=50, want_lse=True, stream=s)
+        few, _, ws2 = lot.lot_window_fwd(one, k, v, left=-1, stream=s)
+        return [out, lse, few, *lot.lot_window_bwd(q, k, v, out, lse, dout, left=50, stream=s)[:3], *lot.lot_cache4_read(cache, table, zero, 300, d=64, stream=s),
+                lot.lot_cache4_attention(q, cache, table, lens, left=90, stream=s)[0]]
+
+    one, zero = q[:, :, :1].contiguous(), torch.zeros(2, device=DEV, dtype=torch.int32)
+    want = calls(None)
+    torch.cuda.synchronize()
+    junk = [torch.empty_like(x) for _ in range(3) for x in want]
+    torch.cuda._sleep(200_000_000)
+    for x in junk:
+        x.fill_(float("nan"))
+    del junk, x
+    got = calls(stream)
+    side.synchronize()
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
 def test_no_queries_no_keys_no_batch():
     for B, nq, nk in itertools.product((0, 1), (0, 5), (0, 5)):
         q, k, v, dout = draw(16, B, 2, 1, nq, nk, 32, F32)
