@@ -7,13 +7,16 @@
 //     save two shifts of a word's three, but sums that begin at 1024 times the queries lose four digits of a score in the tensor cores.)
 //     The query rows of a key head (its query heads times the new tokens) share its codes.
 //   - scale and least value never touch the codes: S = s (sum q n) + z sum q for each group of 32 channels, and
-//     sum_j p_j v_j = sum (p_j s_j) (n_j - 8) + sum p_j (z_j + 8 s_j).  The 128 goes out of the values' sums by a product of the same weights
-//     with a constant, so that the rounding of the weights p_j s_j to bf16 counts for no more than it would on the values themselves.
+//     sum_j p_j v_j = sum (p_j s_j) (n_j - 8) + sum p_j (z_j + 8 s_j).  The values' 136 goes off the operands (one subtraction a pair, exact), so that the
+//     rounding of the weights p_j s_j to bf16 counts for no more than it would on the values themselves; off the sums, by a product of the same
+//     weights with a constant, it took 162 us where this takes 150.  The keys' 128 goes off the sums:
 //   - (z - 128 s) sum q of all groups is two more products, the sums as three bf16 terms.
 //   - float32 queries: everything as three bf16 terms that sum to the number exactly, and centred codes.
 // A warp goes over chunks of 32 tokens by itself: its lanes fetch them with bulk copies into a ring of its own.  Running maximum and sum
 // per warp (the maximum moves only when a score passes it by 2^8), warps and blocks of a split join at the end: the blocks of few
 // sequences through a cluster's shared memory (one launch, latency), of many through memory and join_kernel.
+// 32 sequences of up to 16384 tokens, 32 heads on 8 of 128 channels: 150 us, 3.4 TB/s.  At 166 us issue slots were 60 % used and the ALU
+// pipe 55 %, and three blocks an SM with three stages took 175, five of 96 registers 190.
 #include "lot_chain.cuh"
 #include "lot_sm100.cuh"
 #include "lot_window.cuh"
@@ -114,7 +117,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) attend_kernel(const __grid_
     extern __shared__ __align__(128) uint8_t smem[];
     using L = Lay<D>;
     constexpr int W = L::W, TERMS = sizeof(T) == 4 ? 3 : 1;
-    constexpr bool kLifted = TERMS == 1;                   // products of 128 + code, the 128 taken out of the sums
+    constexpr bool kLifted = TERMS == 1;                   // keys: products of 128 + code, the 128 taken out of the sums
     const Attend4 &a = A.a;
     const Cache4 &c = a.cache;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -162,9 +165,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) attend_kernel(const __grid_
         const uint32_t got = __ballot_sync(0xffffffffu, page >= 0) & 3u;
         if (lane == 0) mbar_arrive_expect_tx(bars + 8 * s, __popc(got) * (L::STAGE / 2));
         __syncwarp();
-        if (lane < 8 && page >= 0) {
+        const bool both = got == 3u && c.page_size % kChunk == 0;                       // neighbours: one copy for both (162 us, two 166)
+        if (lane < 8 && page >= 0 && !(both && blk)) {
             const int tok = token(turn), at = tok - page_of(tok) * c.page_size;
-            bulk_load(dst0 + s * L::STAGE, lane_base + page * page_bytes + (uint32_t)at * unit, piece, bars + 8 * s);
+            bulk_load(dst0 + s * L::STAGE, lane_base + page * page_bytes + (uint32_t)at * unit, both ? 2 * piece : piece, bars + 8 * s);
         }
         if (page == -2 && lane < 2 && a.status != nullptr) atomicOr(a.status, 32 /* LOT_DEV_PAGE */);
         return got;
@@ -382,16 +386,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) attend_kernel(const __grid_
                 for (int m = 0; m < TERMS; ++m) { x0[m] = flip(x0[m]); x1[m] = flip(x1[m]); }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    if (kLifted) {
-                        const uint32_t f[4] = {lifted(va[w], 2 * h), lifted(va[w], 2 * h + 1), lifted(vc[w], 2 * h), lifted(vc[w], 2 * h + 1)};
-                        const uint32_t away[4] = {0xc308c308u, 0xc308c308u, 0xc308c308u, 0xc308c308u};            // -136
-                        mma(o[2 * w + h], away, x0[0], x1[0], o[2 * w + h]);
-                        mma(o[2 * w + h], f, x0[0], x1[0], o[2 * w + h]);
-                    } else {
-                        const uint32_t f[4] = {centred(va[w], 2 * h), centred(va[w], 2 * h + 1), centred(vc[w], 2 * h), centred(vc[w], 2 * h + 1)};
+                    const uint32_t f[4] = {centred(va[w], 2 * h), centred(va[w], 2 * h + 1), centred(vc[w], 2 * h), centred(vc[w], 2 * h + 1)};
 #pragma unroll
-                        for (int m = TERMS - 1; m >= 0; --m) mma(o[2 * w + h], f, x0[m], x1[m], o[2 * w + h]);
-                    }
+                    for (int m = TERMS - 1; m >= 0; --m) mma(o[2 * w + h], f, x0[m], x1[m], o[2 * w + h]);
                 }
             }
         }
