@@ -298,99 +298,99 @@ __global__ void __launch_bounds__(kThreads, 1) bwd_tc_kernel(const __grid_consta
             const bool some = left > 0;
             const f2 l2 = pack2(lse2, lse2), d2 = pack2(dl, dl);
             float sum = 0.f, rounded = 0.f;                // queries: of this row's score gradients, and of what the products take for them
-                for (; ok && left > 0; --left, ++g) {
-                    const int y0 = yt * kTile + col0;
-                    if (++yt == wrap_at) yt = wrap_to;
-                    const uint32_t s = g % P::kYStages;
-                    const uint32_t st = sbase + P::kS + s * P::kStat + 4 * col0;
-                    float p[32];
-                    ok = wait(sbase + P::bS, g);
+            for (; ok && left > 0; --left, ++g) {
+                const int y0 = yt * kTile + col0;
+                if (++yt == wrap_at) yt = wrap_to;
+                const uint32_t s = g % P::kYStages;
+                const uint32_t st = sbase + P::kS + s * P::kStat + 4 * col0;
+                float p[32];
+                ok = wait(sbase + P::bS, g);
+                if (!ok) break;
+                tc_fence_after();
+                tmem_ld32(lanes + P::cS + col0, p);
+                const uint32_t seen = bits_between(lo - y0, hi - y0) | bits_between(-y0, sk - y0);
+                const bool part = __any_sync(0xffffffffu, seen != 0xffffffffu);
+                if constexpr (KEYS) {
+                    ok = wait(sbase + P::bYFull + 8 * s, g / P::kYStages);      // the columns' statistics
                     if (!ok) break;
-                    tc_fence_after();
-                    tmem_ld32(lanes + P::cS + col0, p);
-                    const uint32_t seen = bits_between(lo - y0, hi - y0) | bits_between(-y0, sk - y0);
-                    const bool part = __any_sync(0xffffffffu, seen != 0xffffffffu);
-                    if constexpr (KEYS) {
-                        ok = wait(sbase + P::bYFull + 8 * s, g / P::kYStages);      // the columns' statistics
-                        if (!ok) break;
+                }
+                settle(p);
+                if constexpr (!KEYS) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float u, v;
+                        unpack2(fma2(pack2(p[e], p[e + 1]), c2, l2), u, v);
+                        p[e] = ex2(u);
+                        p[e + 1] = ex2(v);
                     }
-                    settle(p);
-                    if constexpr (!KEYS) {
+                } else {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            float u, v;
-                            unpack2(fma2(pack2(p[e], p[e + 1]), c2, l2), u, v);
-                            p[e] = ex2(u);
-                            p[e + 1] = ex2(v);
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4) {
-                            f2 x, y;
-                            float u, v;
-                            lds2(st + 4 * e, x, y);
-                            unpack2(fma2(pack2(p[e], p[e + 1]), c2, x), u, v);
-                            p[e] = ex2(u);
-                            p[e + 1] = ex2(v);
-                            unpack2(fma2(pack2(p[e + 2], p[e + 3]), c2, y), u, v);
-                            p[e + 2] = ex2(u);
-                            p[e + 3] = ex2(v);
-                        }
+                    for (int e = 0; e < 32; e += 4) {
+                        f2 x, y;
+                        float u, v;
+                        lds2(st + 4 * e, x, y);
+                        unpack2(fma2(pack2(p[e], p[e + 1]), c2, x), u, v);
+                        p[e] = ex2(u);
+                        p[e + 1] = ex2(v);
+                        unpack2(fma2(pack2(p[e + 2], p[e + 3]), c2, y), u, v);
+                        p[e + 2] = ex2(u);
+                        p[e + 3] = ex2(v);
                     }
-                    if (part) {
+                }
+                if (part) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) p[e] = (seen >> e) & 1u ? p[e] : 0.f;
-                    }
-                    {
-                        uint32_t x[16];
+                    for (int e = 0; e < 32; ++e) p[e] = (seen >> e) & 1u ? p[e] : 0.f;
+                }
+                {
+                    uint32_t x[16];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = tile::pack_bf16(p[2 * e], p[2 * e + 1]);
-                        tmem_st16(lanes + P::cS + col0, x);
-                        tmem_wait_st();
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(sbase + P::bW1);
-                    }
-                    ok = wait(sbase + P::bDP, g);
-                    if (!ok) break;
-                    tc_fence_after();
-                    // dP sixteen columns at a time, the next on their way: registers
-                    float dp[2][16];
-                    tmem_ld16(lanes + P::cDP + col0, dp[0]);
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        uint32_t x[8];
-                        settle(dp[k]);
-                        if (k == 0) tmem_ld16(lanes + P::cDP + col0 + 16, dp[1]);
-#pragma unroll
-                        for (int e = 0; e < 16; e += 4) {
-                            const int at = 16 * k + e;
-                            f2 u = d2, v = d2;
-                            if constexpr (KEYS) lds2(st + 4 * (kTile + at), u, v);
-                            u = mul2(pack2(p[at], p[at + 1]), add2(pack2(dp[k][e], dp[k][e + 1]), u));
-                            v = mul2(pack2(p[at + 2], p[at + 3]), add2(pack2(dp[k][e + 2], dp[k][e + 3]), v));
-                            unpack2(u, p[at], p[at + 1]);
-                            unpack2(v, p[at + 2], p[at + 3]);
-                        }
-                        if (part) {                        // not a product with what may be no number
-#pragma unroll
-                            for (int e = 16 * k; e < 16 * k + 16; ++e) p[e] = (seen >> e) & 1u ? p[e] : 0.f;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            x[e] = tile::pack_bf16(p[16 * k + 2 * e], p[16 * k + 2 * e + 1]);
-                            if (!KEYS) {
-                                sum += p[16 * k + 2 * e] + p[16 * k + 2 * e + 1];
-                                rounded += __uint_as_float(x[e] << 16) + __uint_as_float(x[e] & 0xffff0000u);
-                            }
-                        }
-                        tmem_st8(lanes + P::cDP + col0 + 8 * k, x);
-                    }
+                    for (int e = 0; e < 16; ++e) x[e] = tile::pack_bf16(p[2 * e], p[2 * e + 1]);
+                    tmem_st16(lanes + P::cS + col0, x);
                     tmem_wait_st();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(sbase + P::bW2);
+                    if (lane == 0) mbar_arrive(sbase + P::bW1);
                 }
+                ok = wait(sbase + P::bDP, g);
+                if (!ok) break;
+                tc_fence_after();
+                // dP sixteen columns at a time, the next on their way: registers
+                float dp[2][16];
+                tmem_ld16(lanes + P::cDP + col0, dp[0]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    uint32_t x[8];
+                    settle(dp[k]);
+                    if (k == 0) tmem_ld16(lanes + P::cDP + col0 + 16, dp[1]);
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const int at = 16 * k + e;
+                        f2 u = d2, v = d2;
+                        if constexpr (KEYS) lds2(st + 4 * (kTile + at), u, v);
+                        u = mul2(pack2(p[at], p[at + 1]), add2(pack2(dp[k][e], dp[k][e + 1]), u));
+                        v = mul2(pack2(p[at + 2], p[at + 3]), add2(pack2(dp[k][e + 2], dp[k][e + 3]), v));
+                        unpack2(u, p[at], p[at + 1]);
+                        unpack2(v, p[at + 2], p[at + 3]);
+                    }
+                    if (part) {                        // not a product with what may be no number
+#pragma unroll
+                        for (int e = 16 * k; e < 16 * k + 16; ++e) p[e] = (seen >> e) & 1u ? p[e] : 0.f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        x[e] = tile::pack_bf16(p[16 * k + 2 * e], p[16 * k + 2 * e + 1]);
+                        if (!KEYS) {
+                            sum += p[16 * k + 2 * e] + p[16 * k + 2 * e + 1];
+                            rounded += __uint_as_float(x[e] << 16) + __uint_as_float(x[e] & 0xffff0000u);
+                        }
+                    }
+                    tmem_st8(lanes + P::cDP + col0 + 8 * k, x);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sbase + P::bW2);
+            }
             if (ok && some) {
                 ok = wait(sbase + P::bAcc, count++);
                 tc_fence_after();
