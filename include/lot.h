@@ -349,7 +349,8 @@ LOT_API size_t lot_cache4_bytes(int num_pages, int Hkv, int page_size, int d);
 /*
  * lot_cache4_write -- tokens k, v [B,Hkv,m,d] of `dtype` go to positions start[b] .. start[b] + m - 1 of their sequences; with
  * count [B] int32 (or NULL: m) only the first count[b] of them.  Positions outside [0, max_pages * page_size): not written
- * (LOT_DEV_PAGE).  Two tokens of one call must not share a place.
+ * (LOT_DEV_PAGE).  Two tokens of one call must not share a place, and calls that run at once must not write to the same sixteen places (16 i to
+ * 16 i + 15 of a page): neighbours' codes share words.
  */
 LOT_API int lot_cache4_write(const void *k, const void *v, const int32_t *pages, const int32_t *start, const int32_t *count,
                      int dtype, int B, int Hkv, int m, int d, int page_size, int max_pages, int num_pages,
