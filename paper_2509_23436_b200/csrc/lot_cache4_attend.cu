@@ -387,8 +387,15 @@ __global__ void __launch_bounds__(kThreads, kBlocks) attend_kernel(const __grid_
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t f[4] = {centred(va[w], 2 * h), centred(va[w], 2 * h + 1), centred(vc[w], 2 * h), centred(vc[w], 2 * h + 1)};
+                    if (TERMS == 1) {
+                        mma(o[2 * w + h], f, x0[0], x1[0], o[2 * w + h]);
+                    } else {                               // products round their sums towards zero: short ones for float32
+                        float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int m = TERMS - 1; m >= 0; --m) mma(o[2 * w + h], f, x0[m], x1[m], o[2 * w + h]);
+                        for (int m = TERMS - 1; m >= 0; --m) mma(y, f, x0[m], x1[m], y);
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) o[2 * w + h][n] += y[n];
+                    }
                 }
             }
         }
