@@ -315,13 +315,16 @@ __global__ void __launch_bounds__(kThreads, kBlocks) attend_kernel(const __grid_
                 for (int e = 0; e < 4; ++e) S[kb][e] = 0.f;
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
-                    float x[4] = {0.f, 0.f, 0.f, 0.f};
+                    float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};      // y: the small terms
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t f[4] = {centred(ka[w], 2 * h), centred(kc[w], 2 * h), centred(ka[w], 2 * h + 1), centred(kc[w], 2 * h + 1)};
 #pragma unroll
-                        for (int m = TERMS - 1; m >= 0; --m) mma(x, f, qf[m][w][h][0], qf[m][w][h][1], x);
+                        for (int m = TERMS - 1; m > 0; --m) mma(y, f, qf[m][w][h][0], qf[m][w][h][1], y);
+                        mma(x, f, qf[0][w][h][0], qf[0][w][h][1], x);
                     }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] += y[e];
                     const float s0 = param_scale(pa[w]), s1 = param_scale(pc[w]);
                     const float z0 = fmaf(8.f, s0, param_least(pa[w])), z1 = fmaf(8.f, s1, param_least(pc[w]));
                     S[kb][0] = fmaf(s0, x[0], fmaf(z0, qsum[w][0], S[kb][0]));
